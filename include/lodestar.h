@@ -49,6 +49,7 @@ extern "C" {
 
 #define LS_FP32 0   /* fp32 weights and activations */
 #define LS_BF16 1   /* bf16 weights and layer inputs, fp32 accumulation, fp32 master weights */
+#define LS_FP16 2   /* IEEE half: queries, keys, values and outputs of the KV-cache calls only */
 
 #define LS_MAX_HIDDEN 3
 #define LS_DERIVED_COLS 5
@@ -505,13 +506,103 @@ int ls_set_shadow_training(ls_ctx* ctx, int enable, void* stream);
 int ls_swap_model(ls_ctx* ctx, void* serve_stream, void* train_stream);
 
 /*
+ * An instance's paged KV cache in 8 bits (Section 2: an engine keeps the keys
+ * and values of its cached prompt blocks and reuses them for requests that
+ * share the prefix).  The prefix index above says which blocks an instance
+ * holds; these calls fill and read the blocks themselves: a page is one hashed
+ * block (block_tokens, 16 in the evaluated engines) or a run of them, and a
+ * page table with pages shared between sequences is what a prefix hit gives.
+ *
+ * ls_kv_cache  one layer's cache, device memory owned by the caller:
+ *   dtype        LS_KV_INT8 or LS_KV_FP8 (OCP e4m3)
+ *   n_kv_heads   1..1024;  head_dim 64, 128 or 256;  page_tokens 16, 32, 64 or 128
+ *   n_pages      pages in the pool, >= 1 (offsets are 64 bits wide)
+ *   k, v         codes, n_pages * n_kv_heads * page_tokens * head_dim bytes each, 16-byte aligned.
+ *                Page p, head h start at ((p * n_kv_heads + h) * page_tokens) * head_dim;
+ *                inside, tiles of 1,024 bytes in the order [page_tokens / 16][head_dim / 64],
+ *                a tile being [16 tokens][64 dims] for k and [4][64 dims][4 tokens] for v.
+ *   k_scale, v_scale  fp32 [n_pages x n_kv_heads]: one scale for each page and head;
+ *                a code c stands for c * scale.
+ * ls_kv_batch  the sequences of a call and their new tokens (host struct of device arrays):
+ *   n_seqs, n_tokens, pages_stride, max_new   host values; max_new bounds any sequence's new tokens
+ *   dtype        of the 16-bit tensors of the call: LS_BF16 or LS_FP16
+ *   new_off      int32 [n_seqs + 1], 0 = new_off[0] <= ... <= new_off[n_seqs] = n_tokens: sequence b's
+ *                new tokens are rows new_off[b] .. new_off[b+1] of the call's tensors (none: left out)
+ *   past         int32 [n_seqs] >= 0: tokens of the sequence before them; new row j is at position past[b] + j
+ *   pages        int32 [n_seqs x pages_stride]: token t of sequence b is on page pages[b][t / page_tokens].
+ *                An id outside [0, n_pages) is an absent page (e.g. -1, given back): its tokens are
+ *                neither written nor visible.  The same holds past the end of the table.
+ * ls_rope      rotary position table: cos_tab, sin_tab fp32 [n_positions x rotary / 2] (16-byte aligned),
+ *              rotary a multiple of 32 up to head_dim (later dimensions stay as they are); dimension
+ *              pairs are (i, i + rotary / 2), or (2i, 2i + 1) with interleaved != 0.  A token at position
+ *              n_positions or beyond takes the last row.
+ * Tensors are [rows x heads x head_dim], 16-byte aligned, heads and dimensions
+ * dense, with a row stride in elements that is a multiple of 8.
+ *
+ * ls_kv_append  rotates the new keys in fp32 and stores keys and values in 8 bits, and writes the
+ *   rotated queries (q, q_out both NULL: none; q_out may be q).  A page and head's scale is the
+ *   largest magnitude / 127 for LS_KV_INT8 and the smallest power of two that the format's 448 covers
+ *   the largest magnitude with for LS_KV_FP8, clamped to [2^-64, 2^64]; codes are rounded to nearest,
+ *   ties to even.  While a page fills over several calls its scale only grows, and what it holds is
+ *   brought to the new scale: exact for LS_KV_FP8 apart from its subnormals, one more rounding for
+ *   LS_KV_INT8 (so int8 codes can depend on how the tokens were split over calls).  A call whose first
+ *   token opens a page ignores what the page held.  Infinities are stored as the largest code and do
+ *   not count towards the scale; NaN is stored as 0: a cache never holds either.  A page that the call
+ *   writes must be one sequence's alone.
+ * ls_kv_attention  out row t, head h = sum_j softmax_j(scale q . k_j) v_j over the visible tokens j of the
+ *   row's sequence (new ones included: append first), query head h reading kv head
+ *   h / (n_q_heads / n_kv_heads).  Token j is visible at position p when j <= p and, with window > 0,
+ *   j > p - window or j < sinks.  A row that sees nothing gets 0.  Keys and values that no row of a
+ *   16-token block sees are not read; what masked places hold does not reach any result.  Softmax
+ *   statistics and sums are fp32; probabilities enter the products in half precision, scaled by a power of two.
+ * ls_kv_read  rows of 16-bit keys and values (k_out, v_out, dense) that the cache holds for the batch's
+ *   tokens; absent ones read 0.
+ *
+ * All three are asynchronous on `stream`, need neither model nor cache state,
+ * validate on the host, and read device arrays only in bounds whatever these hold.
+ * ls_kv_attention joins work split along long sequences through a workspace of
+ * the context's own, at most LS_KV_WORKSPACE_BYTES, allocated by the first call that
+ * needs it: calls on several streams of one context are ordered by the caller,
+ * and a call to be captured into a graph is made once before.  n_seqs or
+ * n_tokens 0: nothing is done.
+ */
+#define LS_KV_INT8 0
+#define LS_KV_FP8 1
+
+typedef struct {
+    int32_t dtype, n_kv_heads, head_dim, page_tokens;
+    int64_t n_pages;
+    void *k, *v;
+    float *k_scale, *v_scale;
+} ls_kv_cache;
+
+typedef struct {
+    int32_t n_seqs, n_tokens, pages_stride, max_new, dtype;
+    const int32_t *new_off, *past, *pages;
+} ls_kv_batch;
+
+typedef struct {
+    const float *cos_tab, *sin_tab;
+    int32_t n_positions, rotary, interleaved;
+} ls_rope;
+
+int ls_kv_append(ls_ctx* ctx, const ls_kv_cache* cache, const ls_kv_batch* batch, const ls_rope* rope,
+                 const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                 const void* q, int64_t q_stride, int32_t n_q_heads, void* q_out, int64_t q_out_stride, void* stream);
+int ls_kv_attention(ls_ctx* ctx, const ls_kv_cache* cache, const ls_kv_batch* batch, const void* q, int64_t q_stride,
+                    int32_t n_q_heads, float scale, int32_t window, int32_t sinks, void* out, int64_t out_stride,
+                    void* stream);
+int ls_kv_read(ls_ctx* ctx, const ls_kv_cache* cache, const ls_kv_batch* batch, void* k_out, void* v_out, void* stream);
+
+/*
  * Per-kernel timing (the library's own view of where the routing time goes;
  * Section 5.4 measures the router's overhead end to end).  While enabled, each
  * kernel launch group of the context is bracketed by HIP events on the stream
  * of its call (events without a system-scope fence: they order nothing and
  * cost no cache writeback).  Kinds: "table_build", "prefix_match", "instance_partial",
  * "score_pairs", "score_pairs_mfma", "band_select", "rescore", "argmin",
- * "update", "route", "buffer", "index" (prefix-index maintenance).
+ * "update", "route", "buffer", "index" (prefix-index maintenance), "kv_append",
+ * "kv_attention", "kv_read".
  *   ls_profile_enable  enable != 0 starts recording (and clears old records).
  *   ls_profile_read    synchronous; for up to max_kinds kinds writes the kind
  *                      name (static string), the number of launches and the

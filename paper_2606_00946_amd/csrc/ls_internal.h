@@ -368,4 +368,26 @@ hipError_t launch_update(const ModelDims& m, float* master, float* compute, cons
                          float* loss_out, float* grad_out, void* workspace, const DropArgs& drop, int n_cu,
                          hipStream_t s);
 
+// An instance's paged KV cache (k_kv.h): one call's sequences and the cache they live in.
+struct KvView {
+    uint8_t *k, *v;                 // codes
+    float *ks, *vs;                 // [n_pages x H] scales
+    int64_t n_pages;
+    int32_t H, D, page, page_shift; // kv heads, head dimension, tokens of a page and their log2
+    const int32_t *off, *past, *pages;
+    int32_t B, T, W;                // sequences, rows, pages of a table row
+    int32_t max_new;                // no sequence has more rows
+    bool fp8, f16;                  // code type; 16-bit type of the call's tensors
+};
+struct KvRope {
+    const float *cos, *sin;
+    int32_t n_pos, rotary, interleaved;
+};
+hipError_t launch_kv_append(const KvView& c, const KvRope& r, const void* k, int64_t k_stride, const void* v,
+                            int64_t v_stride, const void* q, int64_t q_stride, int32_t Hq, void* q_out,
+                            int64_t q_out_stride, hipStream_t s);
+hipError_t launch_kv_read(const KvView& c, void* k_out, void* v_out, hipStream_t s);
+hipError_t launch_kv_attention(const KvView& c, const void* q, int64_t q_stride, int32_t Hq, float scale,
+                               int32_t window, int32_t sinks, void* out, int64_t out_stride, hipStream_t s);
+
 }  // namespace ls

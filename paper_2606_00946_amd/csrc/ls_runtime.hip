@@ -276,11 +276,11 @@ int grow(ls_ctx* c, void** p, size_t* cap, size_t bytes, hipStream_t s) {
 
 enum Kind {
     K_TABLE = 0, K_PREFIX, K_PARTIAL, K_SCORE, K_ARGMIN, K_UPDATE, K_SCORE_MFMA, K_BAND, K_RESCORE, K_ROUTE, K_BUFFER,
-    K_INDEX, K_COUNT
+    K_INDEX, K_KV_APPEND, K_KV_ATTENTION, K_KV_READ, K_COUNT
 };
 const char* const kKindNames[K_COUNT] = {"table_build", "prefix_match", "instance_partial", "score_pairs", "argmin",
                                          "update", "score_pairs_mfma", "band_select", "rescore", "route",
-                                         "buffer", "index"};
+                                         "buffer", "index", "kv_append", "kv_attention", "kv_read"};
 
 hipEvent_t take_event(ls_ctx* c) {
     if (!c->spare.empty()) {
@@ -1346,6 +1346,165 @@ int ls_train_round(ls_ctx* c, int32_t epochs, int32_t batch, float lr, const int
         LS_TIMED(c, K_UPDATE, s,
                  ls::launch_prepare_mfma(ls::make_mfma_layout(c->dims), TM.master, TM.frag16, TM.frag32, s));
     return LS_OK;
+}
+
+// ---------------------------------------------------------------------------
+// paged 8-bit KV cache
+// ---------------------------------------------------------------------------
+}  // extern "C"
+
+namespace {
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+// Checks the descriptors every KV call takes and turns them into the kernels' view.
+int kv_view(ls_ctx* c, const ls_kv_cache* kv, const ls_kv_batch* b, ls::KvView* out) {
+    if (!kv || !b) return fail(c, LS_ERR_INVALID, "cache and batch must be non-NULL");
+    if (kv->dtype != LS_KV_INT8 && kv->dtype != LS_KV_FP8)
+        return fail(c, LS_ERR_INVALID, "cache dtype must be LS_KV_INT8 or LS_KV_FP8");
+    if (b->dtype != LS_BF16 && b->dtype != LS_FP16)
+        return fail(c, LS_ERR_INVALID, "batch dtype must be LS_BF16 or LS_FP16");
+    if (kv->n_kv_heads < 1 || kv->n_kv_heads > 1024) return fail(c, LS_ERR_INVALID, "n_kv_heads must be 1..1024");
+    if (kv->head_dim != 64 && kv->head_dim != 128 && kv->head_dim != 256)
+        return fail(c, LS_ERR_INVALID, "head_dim must be 64, 128 or 256");
+    if (kv->page_tokens != 16 && kv->page_tokens != 32 && kv->page_tokens != 64 && kv->page_tokens != 128)
+        return fail(c, LS_ERR_INVALID, "page_tokens must be 16, 32, 64 or 128");
+    if (kv->n_pages < 1 || kv->n_pages > INT32_MAX) return fail(c, LS_ERR_INVALID, "n_pages must be 1..2^31 - 1");
+    if (!kv->k || !kv->v || !kv->k_scale || !kv->v_scale)
+        return fail(c, LS_ERR_INVALID, "the cache's arrays must be non-NULL");
+    if (!aligned16(kv->k) || !aligned16(kv->v)) return fail(c, LS_ERR_INVALID, "k and v must be 16-byte aligned");
+    if (b->n_seqs < 0 || b->n_tokens < 0) return fail(c, LS_ERR_INVALID, "n_seqs and n_tokens must be >= 0");
+    if (b->n_seqs > 0 && b->n_tokens > 0) {
+        if (!b->new_off || !b->past || !b->pages)
+            return fail(c, LS_ERR_INVALID, "new_off, past and pages must be non-NULL");
+        if (b->pages_stride < 1) return fail(c, LS_ERR_INVALID, "pages_stride must be >= 1");
+        if (b->max_new < 1) return fail(c, LS_ERR_INVALID, "max_new must be >= 1");
+    }
+    ls::KvView v;
+    v.k = (uint8_t*)kv->k;
+    v.v = (uint8_t*)kv->v;
+    v.ks = kv->k_scale;
+    v.vs = kv->v_scale;
+    v.n_pages = kv->n_pages;
+    v.H = kv->n_kv_heads;
+    v.D = kv->head_dim;
+    v.page = kv->page_tokens;
+    v.page_shift = __builtin_ctz((unsigned)kv->page_tokens);
+    v.off = b->new_off;
+    v.past = b->past;
+    v.pages = b->pages;
+    v.B = b->n_seqs;
+    v.T = b->n_tokens;
+    v.W = b->pages_stride;
+    v.max_new = std::min(b->max_new, b->n_tokens);
+    v.fp8 = kv->dtype == LS_KV_FP8;
+    v.f16 = b->dtype == LS_FP16;
+    *out = v;
+    return LS_OK;
+}
+
+// A call's tensor of `heads` heads a row.
+int kv_tensor(ls_ctx* c, const char* name, const void* p, int64_t stride, int64_t heads, int32_t D) {
+    if (!p) return fail(c, LS_ERR_INVALID, "%s must be non-NULL", name);
+    if (!aligned16(p)) return fail(c, LS_ERR_INVALID, "%s must be 16-byte aligned", name);
+    if (stride < heads * D || stride % 8)
+        return fail(c, LS_ERR_INVALID, "%s_stride must be a multiple of 8 and at least heads * head_dim", name);
+    return LS_OK;
+}
+
+int kv_q_heads(ls_ctx* c, int32_t Hq, int32_t H) {
+    if (Hq < 1 || Hq % H || Hq / H > 1024)
+        return fail(c, LS_ERR_INVALID, "n_q_heads must be a multiple of n_kv_heads, 1..1024 for each");
+    return LS_OK;
+}
+
+int kv_launched(ls_ctx* c, hipError_t e) {
+    if (e == hipErrorInvalidConfiguration) return fail(c, LS_ERR_UNSUPPORTED, "the batch is too large for one launch");
+    LS_HIP(c, e);
+    return LS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ls_kv_append(ls_ctx* c, const ls_kv_cache* cache, const ls_kv_batch* batch, const ls_rope* rope, const void* k,
+                 int64_t k_stride, const void* v, int64_t v_stride, const void* q, int64_t q_stride,
+                 int32_t n_q_heads, void* q_out, int64_t q_out_stride, void* stream) {
+    if (!c) return LS_ERR_INVALID;
+    c->err.clear();
+    ls::KvView w;
+    int rc = kv_view(c, cache, batch, &w);
+    if (rc) return rc;
+    ls::KvRope r{nullptr, nullptr, 1, 0, 0};
+    if (rope) {
+        if (!rope->cos_tab || !rope->sin_tab) return fail(c, LS_ERR_INVALID, "cos_tab and sin_tab must be non-NULL");
+        if (!aligned16(rope->cos_tab) || !aligned16(rope->sin_tab))
+            return fail(c, LS_ERR_INVALID, "cos_tab and sin_tab must be 16-byte aligned");
+        if (rope->n_positions < 1) return fail(c, LS_ERR_INVALID, "n_positions must be >= 1");
+        if (rope->rotary < 32 || rope->rotary > w.D || rope->rotary % 32)
+            return fail(c, LS_ERR_INVALID, "rotary must be a multiple of 32 in [32, head_dim]");
+        r = {rope->cos_tab, rope->sin_tab, rope->n_positions, rope->rotary, rope->interleaved};
+    }
+    if ((q == nullptr) != (q_out == nullptr)) return fail(c, LS_ERR_INVALID, "q and q_out go together");
+    if (q && (rc = kv_q_heads(c, n_q_heads, w.H))) return rc;
+    if (w.B == 0 || w.T == 0) return LS_OK;
+    if ((rc = kv_tensor(c, "k", k, k_stride, w.H, w.D)) || (rc = kv_tensor(c, "v", v, v_stride, w.H, w.D))) return rc;
+    if (q && ((rc = kv_tensor(c, "q", q, q_stride, n_q_heads, w.D)) ||
+              (rc = kv_tensor(c, "q_out", q_out, q_out_stride, n_q_heads, w.D))))
+        return rc;
+    DeviceScope dev(c->device);
+    if (!dev.ok) return fail(c, LS_ERR_DEVICE, "cannot select device %d", c->device);
+    hipStream_t s = (hipStream_t)stream;
+    Timed t(c, K_KV_APPEND, s);
+    const hipError_t e =
+        ls::launch_kv_append(w, r, k, k_stride, v, v_stride, q, q_stride, n_q_heads, q_out, q_out_stride, s);
+    t.done();
+    return kv_launched(c, e);
+}
+
+int ls_kv_attention(ls_ctx* c, const ls_kv_cache* cache, const ls_kv_batch* batch, const void* q, int64_t q_stride,
+                    int32_t n_q_heads, float scale, int32_t window, int32_t sinks, void* out, int64_t out_stride,
+                    void* stream) {
+    if (!c) return LS_ERR_INVALID;
+    c->err.clear();
+    ls::KvView w;
+    int rc = kv_view(c, cache, batch, &w);
+    if (rc || (rc = kv_q_heads(c, n_q_heads, w.H))) return rc;
+    if (!std::isfinite(scale)) return fail(c, LS_ERR_INVALID, "scale must be finite");
+    if (window < 0 || sinks < 0) return fail(c, LS_ERR_INVALID, "window and sinks must be >= 0");
+    if (w.B == 0 || w.T == 0) return LS_OK;
+    if ((rc = kv_tensor(c, "q", q, q_stride, n_q_heads, w.D)) ||
+        (rc = kv_tensor(c, "out", out, out_stride, n_q_heads, w.D)))
+        return rc;
+    DeviceScope dev(c->device);
+    if (!dev.ok) return fail(c, LS_ERR_DEVICE, "cannot select device %d", c->device);
+    hipStream_t s = (hipStream_t)stream;
+    Timed t(c, K_KV_ATTENTION, s);
+    const hipError_t e =
+        ls::launch_kv_attention(w, q, q_stride, n_q_heads, scale, window, sinks, out, out_stride, s);
+    t.done();
+    return kv_launched(c, e);
+}
+
+int ls_kv_read(ls_ctx* c, const ls_kv_cache* cache, const ls_kv_batch* batch, void* k_out, void* v_out,
+               void* stream) {
+    if (!c) return LS_ERR_INVALID;
+    c->err.clear();
+    ls::KvView w;
+    int rc = kv_view(c, cache, batch, &w);
+    if (rc) return rc;
+    if (w.B == 0 || w.T == 0) return LS_OK;
+    const int64_t row = (int64_t)w.H * w.D;
+    if ((rc = kv_tensor(c, "k_out", k_out, row, w.H, w.D)) || (rc = kv_tensor(c, "v_out", v_out, row, w.H, w.D)))
+        return rc;
+    DeviceScope dev(c->device);
+    if (!dev.ok) return fail(c, LS_ERR_DEVICE, "cannot select device %d", c->device);
+    hipStream_t s = (hipStream_t)stream;
+    Timed t(c, K_KV_READ, s);
+    const hipError_t e = ls::launch_kv_read(w, k_out, v_out, s);
+    t.done();
+    return kv_launched(c, e);
 }
 
 int ls_profile_enable(ls_ctx* c, int enable) {

@@ -17,7 +17,8 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "liblodestar.so")
 
 LS_OK, LS_ERR_INVALID, LS_ERR_NOMEM, LS_ERR_DEVICE, LS_ERR_STATE, LS_ERR_UNSUPPORTED = 0, -1, -2, -3, -4, -5
-LS_FP32, LS_BF16 = 0, 1
+LS_FP32, LS_BF16, LS_FP16 = 0, 1, 2
+LS_KV_INT8, LS_KV_FP8 = 0, 1
 DERIVED_COLS = 5
 _DTYPES = {"fp32": LS_FP32, "f32": LS_FP32, "bf16": LS_BF16}
 
@@ -58,6 +59,23 @@ def make_policy(heuristic=LS_HEUR_PREFIX_LOAD, count_cols=(-1, -1), theta_imbal=
                   delta)
     p._bounds = (lo_a, hi_a)
     return p
+
+
+class ls_kv_cache(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_tokens", ctypes.c_int32), ("n_pages", ctypes.c_int64), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class ls_kv_batch(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_tokens", ctypes.c_int32), ("pages_stride", ctypes.c_int32),
+                ("max_new", ctypes.c_int32), ("dtype", ctypes.c_int32), ("new_off", ctypes.c_void_p),
+                ("past", ctypes.c_void_p), ("pages", ctypes.c_void_p)]
+
+
+class ls_rope(ctypes.Structure):
+    _fields_ = [("cos_tab", ctypes.c_void_p), ("sin_tab", ctypes.c_void_p), ("n_positions", ctypes.c_int32),
+                ("rotary", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
 
 
 _lib = None
@@ -105,6 +123,10 @@ def library():
         lib.ls_score_batch_noalloc.argtypes = [P, i32, i32, P, P, P, P, P, P, P, P, P, P]
         lib.ls_set_cu_limit.argtypes = [P, ctypes.c_int]
         lib.ls_set_chain_kernels.argtypes = [P, ctypes.c_int]
+        kvp, kbp = ctypes.POINTER(ls_kv_cache), ctypes.POINTER(ls_kv_batch)
+        lib.ls_kv_append.argtypes = [P, kvp, kbp, ctypes.POINTER(ls_rope), P, i64, P, i64, P, i64, i32, P, i64, P]
+        lib.ls_kv_attention.argtypes = [P, kvp, kbp, P, i64, i32, f32, i32, i32, P, i64, P]
+        lib.ls_kv_read.argtypes = [P, kvp, kbp, P, P, P]
         for f in (lib.ls_create, lib.ls_set_model, lib.ls_get_model, lib.ls_load_cache_state, lib.ls_score_batch,
                   lib.ls_update, lib.ls_profile_enable, lib.ls_profile_read, lib.ls_set_exact_scores,
                   lib.ls_set_prefix_join, lib.ls_route_batch, lib.ls_set_prefix_closed, lib.ls_buffer_init,
@@ -112,7 +134,7 @@ def library():
                   lib.ls_set_cache_capacity, lib.ls_commit_routes, lib.ls_read_cache_state, lib.ls_set_dropout,
                   lib.ls_set_shadow_training, lib.ls_swap_model, lib.ls_fast_scores, lib.ls_set_cu_limit,
                   lib.ls_set_chain_kernels,
-                  lib.ls_score_batch_noalloc):
+                  lib.ls_score_batch_noalloc, lib.ls_kv_append, lib.ls_kv_attention, lib.ls_kv_read):
             f.restype = ctypes.c_int
         _lib = lib
     return _lib
@@ -172,6 +194,92 @@ def _host(a, dtype, numel=None):
     if numel is not None and a.size != numel:
         raise ValueError(f"expected {numel} elements, got {a.size}")
     return a, a.ctypes.data_as(ctypes.c_void_p)
+
+
+class KVCache:
+    """One layer's paged 8-bit KV cache: its tensors and their ls_kv_cache.
+
+    dtype "int8" or "fp8".  buffers: (k, v, k_scale, v_scale) to use instead of new ones, codes of any 8-bit
+    dtype with n_pages * n_kv_heads * page_tokens * head_dim elements, scales float32 with n_pages * n_kv_heads.
+    """
+
+    def __init__(self, n_pages, n_kv_heads, head_dim, dtype="fp8", page_tokens=16, device=None, buffers=None):
+        import torch
+        if dtype not in ("int8", "fp8"):
+            raise ValueError(f"dtype is {dtype!r}, expected 'int8' or 'fp8'")
+        codes, scales = n_pages * n_kv_heads * page_tokens * head_dim, n_pages * n_kv_heads
+        if buffers is None:
+            device = torch.cuda.current_device() if device is None else device
+            z = lambda n, t: torch.zeros(n, dtype=t, device=device)  # noqa: E731
+            buffers = (z(codes, torch.uint8), z(codes, torch.uint8), z(scales, torch.float32), z(scales, torch.float32))
+        self.k, self.v, self.k_scale, self.v_scale = buffers
+        eight = (torch.uint8, torch.int8, torch.float8_e4m3fn)
+        self.n_kv_heads, self.head_dim = int(n_kv_heads), int(head_dim)
+        self.c = ls_kv_cache(LS_KV_FP8 if dtype == "fp8" else LS_KV_INT8, self.n_kv_heads, self.head_dim,
+                             int(page_tokens), int(n_pages), _dev(self.k, "k", eight, codes),
+                             _dev(self.v, "v", eight, codes), _dev(self.k_scale, "k_scale", (torch.float32,), scales),
+                             _dev(self.v_scale, "v_scale", (torch.float32,), scales))
+        self.ref = ctypes.byref(self.c)
+
+
+class KVBatch:
+    """The sequences of a KV-cache call (ls_kv_batch): new_off int32 [B+1], past int32 [B], pages int32 [B x stride]
+    on the device, and two host values: n_tokens = new_off[B], and max_new, which bounds each sequence's new tokens
+    (default: n_tokens).  The tensors may be refilled between calls: the kernels read them on the stream."""
+
+    def __init__(self, new_off, past, pages, n_tokens, max_new=None):
+        import torch
+        i32 = (torch.int32,)
+        B = past.numel()
+        if pages.dim() != 2 or pages.shape[0] != B:
+            raise ValueError(f"pages must be [{B} x stride]")
+        self.new_off, self.past, self.pages = new_off, past, pages
+        self.n_tokens = int(n_tokens)
+        self.c = ls_kv_batch(B, self.n_tokens, pages.shape[1], int(self.n_tokens if max_new is None else max_new), 0,
+                             _dev(new_off, "new_off", i32, B + 1), _dev(past, "past", i32), _dev(pages, "pages", i32))
+        self.ref = ctypes.byref(self.c)
+
+
+class Rope:
+    """Rotary position table (ls_rope): cos, sin float32 [n_positions x rotary / 2]."""
+
+    def __init__(self, cos, sin, interleaved=False):
+        import torch
+        if cos.dim() != 2 or cos.shape != sin.shape:
+            raise ValueError("cos and sin must be [n_positions x rotary / 2]")
+        self.cos, self.sin = cos, sin
+        self.c = ls_rope(_dev(cos, "cos", (torch.float32,)), _dev(sin, "sin", (torch.float32,)), cos.shape[0],
+                         2 * cos.shape[1], int(bool(interleaved)))
+        self.ref = ctypes.byref(self.c)
+
+
+_LS_16 = {}
+
+
+def _rows(t, name, batch, D, heads=None, like=None):
+    """(pointer, row stride, heads) of a [rows x heads x D] 16-bit tensor whose heads and dimensions are dense."""
+    if not _LS_16:
+        import torch
+        _LS_16.update({torch.bfloat16: LS_BF16, torch.float16: LS_FP16})
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    kind = _LS_16.get(t.dtype)
+    if kind is None:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected bfloat16 or float16")
+    if like is not None and t.dtype != like.dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {like.dtype}")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [rows x heads x {D}]")
+    n, h, d = t.shape
+    if n != batch.n_tokens or d != D or (heads is not None and h != heads):
+        raise ValueError(f"{name} is {tuple(t.shape)}, expected [{batch.n_tokens} x {heads or 'heads'} x {D}]")
+    batch.c.dtype = kind
+    if n == 0:
+        return None, h * D, h
+    s = t.stride()
+    if s[2] != 1 or (h > 1 and s[1] != D):
+        raise ValueError(f"{name}'s heads and dimensions must be dense")
+    return t.data_ptr(), s[0] if n > 1 else h * D, h
 
 
 class Context:
@@ -432,13 +540,50 @@ class Context:
     def ls_set_prefix_join(self, mode=0):
         return self._check("ls_set_prefix_join", self.lib.ls_set_prefix_join(self.h, int(mode)))
 
+    # -- paged 8-bit KV cache ----------------------------------------------
+    def ls_kv_append(self, cache, batch, k, v, rope=None, q=None, q_out=None, stream=None):
+        """Appends rotated keys and values [T x kv heads x D]; q_out gets the rotated queries q (both or neither)."""
+        D, H = cache.head_dim, cache.n_kv_heads
+        kp, ks, _ = _rows(k, "k", batch, D, H)
+        vp, vs, _ = _rows(v, "v", batch, D, H, k)
+        qp = op = None
+        qs = os_ = qh = 0
+        if q is not None or q_out is not None:
+            if q is None or q_out is None:
+                raise ValueError("q and q_out go together")
+            qp, qs, qh = _rows(q, "q", batch, D, like=k)
+            op, os_, _ = _rows(q_out, "q_out", batch, D, qh, k)
+        return self._check("ls_kv_append",
+                           self.lib.ls_kv_append(self.h, cache.ref, batch.ref, None if rope is None else rope.ref,
+                                                 kp, ks, vp, vs, qp, qs, qh, op, os_, _stream(stream)))
+
+    def ls_kv_attention(self, cache, batch, q, out, scale=None, window=0, sinks=0, stream=None):
+        """out [T x q heads x D]: attention of the batch's rows over the cache; scale defaults to 1 / sqrt(D)."""
+        D = cache.head_dim
+        qp, qs, qh = _rows(q, "q", batch, D)
+        op, os_, _ = _rows(out, "out", batch, D, qh, q)
+        return self._check("ls_kv_attention",
+                           self.lib.ls_kv_attention(self.h, cache.ref, batch.ref, qp, qs, qh,
+                                                    D ** -0.5 if scale is None else scale, window, sinks, op, os_,
+                                                    _stream(stream)))
+
+    def ls_kv_read(self, cache, batch, k_out, v_out, stream=None):
+        """The keys and values [T x kv heads x D] that the cache holds for the batch's tokens."""
+        D, H = cache.head_dim, cache.n_kv_heads
+        for t, name in ((k_out, "k_out"), (v_out, "v_out")):
+            if not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+        kp, _, _ = _rows(k_out, "k_out", batch, D, H)
+        vp, _, _ = _rows(v_out, "v_out", batch, D, H, k_out)
+        return self._check("ls_kv_read", self.lib.ls_kv_read(self.h, cache.ref, batch.ref, kp, vp, _stream(stream)))
+
     # -- per-kernel timing ------------------------------------------------
     def ls_profile_enable(self, enable=True):
         return self._check("ls_profile_enable", self.lib.ls_profile_enable(self.h, 1 if enable else 0))
 
     def ls_profile_read(self) -> dict:
         """{kind: (launches, total_ms)} since profiling was enabled (synchronous)."""
-        k = 16
+        k = 32
         names = (ctypes.c_char_p * k)()
         launches = (ctypes.c_int64 * k)()
         ms = (ctypes.c_double * k)()
