@@ -97,6 +97,29 @@ __device__ __forceinline__ float scale_of(float a) {
     return fminf(fmaxf(s, kScaleMin), kScaleMax);
 }
 
+// Four codes of a dword in half precision: exact, every code is a half value.
+template <bool FP8>
+__device__ __forceinline__ half4 code_halves(uint32_t w) {
+    if constexpr (FP8) {
+        const half2v a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, false);
+        const half2v b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, true);
+        return half4{a.x, a.y, b.x, b.y};
+    } else {
+        // 0x6400 | u is 1024 + u: the biased code as a half's mantissa, then the bias and the 1024 off
+        const uint32_t u = w ^ 0x80808080u;
+        const half2v off = {(_Float16)1152.0f, (_Float16)1152.0f};
+        const half2v a = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) - off;
+        const half2v b = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) - off;
+        return half4{a.x, a.y, b.x, b.y};
+    }
+}
+
+template <bool FP8>
+__device__ __forceinline__ half8 code_halves8(uint32_t lo, uint32_t hi) {
+    const half4 a = code_halves<FP8>(lo), b = code_halves<FP8>(hi);
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
 // ---- addresses -------------------------------------------------------------------
 // Byte offset of 16-token block `blk` of a page and head.
 __device__ __forceinline__ int64_t block_at(const KvView& c, int64_t page, int h, int blk) {
@@ -132,6 +155,20 @@ __device__ __forceinline__ int seq_of_slot(const KvView& c, int64_t slot, F firs
         n = min(step, n - k * step);
     }
     return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// A value that is the same in every lane, for the compiler too.
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x);
+    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)x >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+// A value that is the same in every lane, from read-only memory through the scalar cache.
+template <class T>
+__device__ __forceinline__ T uniform_load(const T* p) {
+    using C = const __attribute__((address_space(4))) T;
+    return *(C*)(uintptr_t)p;
 }
 
 __device__ __forceinline__ float wave_max(float x) {

@@ -83,6 +83,9 @@ struct ls_ctx {
     // shares memory with a scoring call on another stream
     void* upd_ws = nullptr;
     size_t upd_ws_cap = 0;
+    // partial sums of ls_kv_attention's split rows
+    void* kv_ws = nullptr;
+    size_t kv_ws_cap = 0;
     // online-learning data path (device pools, host-side counters)
     struct Buffer {
         int32_t fifo_cap = 0, rep_cap = 0, fifo_count = 0, fifo_head = 0, rep_count = 0;
@@ -473,7 +476,7 @@ void ls_destroy(ls_ctx* c) {
                         (void*)c->buf.fifo_y, (void*)c->buf.rep_x, (void*)c->buf.rep_y, (void*)c->buf.emb,
                         (void*)c->buf.D, c->buf.ws, (void*)c->idx.hash,
                         (void*)c->idx.stamp, (void*)c->idx.hash2, (void*)c->idx.stamp2, (void*)c->idx.entry_of,
-                        (void*)c->idx.small, c->idx.ws, (void*)c->sh_master, (void*)c->sh_compute, c->upd_ws,
+                        (void*)c->idx.small, c->idx.ws, (void*)c->sh_master, (void*)c->sh_compute, c->upd_ws, c->kv_ws,
                         (void*)c->sh_frag16, (void*)c->sh_frag32})
             if (p) (void)hipFree(p);
         if (c->stage) (void)hipHostFree(c->stage);
@@ -1480,9 +1483,12 @@ int ls_kv_attention(ls_ctx* c, const ls_kv_cache* cache, const ls_kv_batch* batc
     DeviceScope dev(c->device);
     if (!dev.ok) return fail(c, LS_ERR_DEVICE, "cannot select device %d", c->device);
     hipStream_t s = (hipStream_t)stream;
+    if (ls::kv_attention_workspace_bytes(w, c->n_cu_dev) > LS_KV_WORKSPACE_BYTES)
+        return fail(c, LS_ERR_UNSUPPORTED, "the batch is too large for the workspace");
+    if ((rc = grow(c, &c->kv_ws, &c->kv_ws_cap, LS_KV_WORKSPACE_BYTES, s))) return rc;
     Timed t(c, K_KV_ATTENTION, s);
-    const hipError_t e =
-        ls::launch_kv_attention(w, q, q_stride, n_q_heads, scale, window, sinks, out, out_stride, s);
+    const hipError_t e = ls::launch_kv_attention(w, q, q_stride, n_q_heads, scale, window, sinks, out, out_stride,
+                                                 c->kv_ws, c->n_cu, s);
     t.done();
     return kv_launched(c, e);
 }
