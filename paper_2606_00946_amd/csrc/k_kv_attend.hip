@@ -11,7 +11,10 @@
 // rounding of the probabilities); codes and 16-bit queries are exact there, a
 // bf16 query after scaling its row by a power of two.  The maximum, the sums and
 // the products are fp32.
+#include <algorithm>
+
 #include "k_kv.h"
+#include "ls_scratch.h"
 
 namespace ls {
 namespace {
@@ -51,6 +54,23 @@ __device__ __forceinline__ Span span_of(const KvView& c, const AttnArgs& a, int6
     return s;
 }
 
+// Which of a block's 16 tokens a row sees: up to `last`, and those after `gone` or
+// before `sink`.  Bounds are relative to the block, so 32 bits do; the tests are
+// joined without branches.
+struct Sight {
+    int32_t last, gone, sink;
+    __device__ __forceinline__ bool sees(int i) const { return (i <= last) & ((i > gone) | (i < sink)); }
+};
+__device__ __forceinline__ Sight sight(const AttnArgs& a, int32_t page, int64_t pos, int64_t tok) {
+    auto near = [](int64_t x) { return (int32_t)min(max(x, (int64_t)-1), (int64_t)16); };
+    Sight s;
+    s.last = page < 0 ? -1 : near(pos - tok);
+    s.gone = a.window > 0 ? near(pos - a.window - tok) : -1;
+    s.sink = near(a.sinks - tok);
+    return s;
+}
+
+constexpr int kFewRows = 16;         // rows of a kv head that kv_split_kernel takes
 constexpr int kUnit = 8;             // 16-token blocks of a work unit: two for each wave of a workgroup
 constexpr float kNoMax = -1e30f;     // running maximum of nothing
 constexpr float kTop = 7.0f;         // weights start below 2^7 ...
@@ -63,6 +83,16 @@ __device__ __forceinline__ int32_t units_of(const KvView& c, const AttnArgs& a, 
     if (n == 0 || (int64_t)n * a.G > a.few) return 0;
     const Span s = span_of(c, a, max(c.past[b], 0), n);
     return max((s.n + kUnit - 1) / kUnit, 1);
+}
+
+// Power of two that brings a row of bf16 queries whose largest magnitude has the
+// bits `top` below 2^14, and its reciprocal.  Above 2^-100 only: smaller rows
+// round to zero scores in fp32 anyway.
+__device__ __forceinline__ float half_range_factor(uint32_t top) {
+    return __uint_as_float((uint32_t)(267 - max((int)(top >> 23), 27)) << 23);
+}
+__device__ __forceinline__ float half_range_undo(uint32_t top) {
+    return __uint_as_float((uint32_t)(max((int)(top >> 23), 27) - 13) << 23);
 }
 
 // Rows of a kv head (new token, then query head) as 16 columns: a column's query
@@ -96,8 +126,7 @@ __device__ __forceinline__ float load_queries(const AttnArgs& a, int D_heads_h, 
                     top = max(top, max((raw[dt][s][i] << 16) & 0x7FFFFFFFu, raw[dt][s][i] & 0x7FFF0000u));
         top = max(top, (uint32_t)__shfl_xor((int)top, 16));
         top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-        const int e = max((int)(top >> 23), 27);                // biased: the row's largest is below 2^(e - 126)
-        const float f = __uint_as_float((uint32_t)(min(267 - e, 254)) << 23);     // 2^(140 - e): below 2^14 and up
+        const float f = half_range_factor(top);
 #pragma unroll
         for (int dt = 0; dt < D / 64; ++dt)
 #pragma unroll
@@ -108,7 +137,7 @@ __device__ __forceinline__ float load_queries(const AttnArgs& a, int D_heads_h, 
                     q[dt][s][2 * i] = (_Float16)(x.x * f);
                     q[dt][s][2 * i + 1] = (_Float16)(x.y * f);
                 }
-        return __uint_as_float((uint32_t)(254 - min(267 - e, 254)) << 23);
+        return half_range_undo(top);
     }
 }
 
@@ -256,12 +285,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_split_kernel(KvView 
 #pragma unroll
                     for (int k = 0; k < 4; ++k) x[e][k] = fmaf(s[k], f, lv);
                 } else {
+                    const Sight see = sight(a, m.page[e], pos, tok);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int64_t j = tok + 4 * g + k;
-                        const bool see = m.page[e] >= 0 && j <= pos && (a.window == 0 || j > pos - a.window || j < a.sinks);
-                        x[e][k] = see ? fmaf(s[k], f, lv) : -INFINITY;
-                    }
+                    for (int k = 0; k < 4; ++k) x[e][k] = see.sees(4 * g + k) ? fmaf(s[k], f, lv) : -INFINITY;
                     // codes of nobody's tokens may be NaN: out of the product
                     const int64_t left = m.page[e] >= 0 ? end_tok - (tok + 4 * g) : 0;
                     const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * (int)left)) - 1;
@@ -406,85 +432,344 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvView c, AttnArgs a) {
             uint2v{pack2<F16>(v[dt].x * norm, v[dt].y * norm), pack2<F16>(v[dt].z * norm, v[dt].w * norm)};
 }
 
-// One wave per row and query head; 64 keys at a time, a lane each.
-template <bool FP8, bool F16>
-__global__ __launch_bounds__(256) void kv_attend_kernel(KvView c, const uint16_t* __restrict__ q, int64_t q_stride,
-                                                        int32_t Hq, float scale, int32_t window, int32_t sinks,
-                                                        uint16_t* __restrict__ out, int64_t out_stride, int32_t few) {
-    __shared__ float qs[4][256];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)blockIdx.x * 4 + wave;
-    if (w >= (int64_t)c.T * Hq) return;
-    const int hq = (int)(w % Hq), t = (int)(w / Hq);
-    const int h = hq / (Hq / c.H);
-    int lo = 0, n = c.B;
-    while (n > 1) {
-        const int m = n >> 1;
-        if (min(max(c.off[lo + m], 0), c.T) <= t) { lo += m; n -= m; } else { n = m; }
-    }
-    const int b = lo;
-    if ((int64_t)(min(max(c.off[b + 1], 0), c.T) - min(max(c.off[b], 0), c.T)) * (Hq / c.H) <= few) return;
-    const int64_t pos = (int64_t)max(c.past[b], 0) + t - min(max(c.off[b], 0), c.T);
-    for (int d = lane; d < c.D; d += 64) {
-        const uint16_t u = q[t * q_stride + (int64_t)hq * c.D + d];
-        qs[wave][d] = unpack2<F16>(u).x;
-    }
-    __builtin_amdgcn_wave_barrier();
-    const int nd = c.D >> 6;
-    float m = -INFINITY, l = 0.0f, o[4] = {0, 0, 0, 0};
-    const int64_t end = min(pos + 1, (int64_t)c.W << c.page_shift);
-    for (int64_t j0 = 0; j0 < end; j0 += 64) {
-        const int64_t j = j0 + lane;
-        const bool seen = j < end && (window <= 0 || j > pos - window || j < sinks);
-        const int64_t page = seen ? page_id(c, b, (int)(j >> c.page_shift)) : -1;
-        if (__ballot(page >= 0) == 0) continue;
-        const int r = (int)j & (c.page - 1);
-        float x = -INFINITY, vs = 0.0f;
-        if (page >= 0) {
-            const uint8_t* tk = c.k + block_at(c, page, h, r >> 4) + (r & 15) * 64;
-            float acc = 0.0f;
-            for (int dt = 0; dt < nd; ++dt)
-                for (int d = 0; d < 64; d += 4) {
-                    const float4v f = code_values<FP8>(*reinterpret_cast<const uint32_t*>(tk + dt * 1024 + d));
-                    for (int i = 0; i < 4; ++i) acc = fmaf(f[i], qs[wave][dt * 64 + d + i], acc);
+// Many rows (prompts): bound by the matrix cores and the exponentials.  A
+// workgroup takes kTileRows rows (new tokens x query heads of one kv head, so
+// that the group's heads share what is staged) and walks the cache 64 tokens at a
+// time: codes become halves on their way into LDS, in the order in which the
+// 32x32x16 products read them (a wave's operand is 1 KB in a row, no bank is hit
+// twice), double-buffered, with the next codes in flight.  Scores are transposed
+// (tokens x rows): their registers are the second operand of the product with the
+// values.  Few tiles: `splits` workgroups share a tile's tokens and
+// kv_tile_join_kernel adds their sums.
+constexpr int kTileRows = 128;
+
+using float16v = float __attribute__((ext_vector_type(16)));
+
+// What a tile's rows [r0, r0 + rows) of sequence b see, 64 tokens a step; the share of split `sp` of `splits`.
+struct TileWork {
+    Span span;
+    int32_t u0, u1, shares;
+};
+__device__ __forceinline__ TileWork tile_work(const KvView& c, const AttnArgs& a, int64_t past, int r0, int rows,
+                                              int sp, int splits) {
+    const int tok0 = r0 / a.G, tok1 = (r0 + rows - 1) / a.G;
+    TileWork w;
+    w.span = span_of(c, a, past + tok0, tok1 - tok0 + 1);
+    const int steps = (w.span.n + 3) >> 2;
+    w.shares = min(splits, max(steps >> 2, 1));      // no share below four steps
+    w.u0 = sp < w.shares ? (int)((int64_t)steps * sp / w.shares) : 0;
+    w.u1 = sp < w.shares ? (int)((int64_t)steps * (sp + 1) / w.shares) : 0;
+    return w;
+}
+
+// The tile of slot `slot`: sequence, its rows' start and count (0: none, or few enough for kv_split_kernel).
+__device__ __forceinline__ int tile_of_slot(const KvView& c, const AttnArgs& a, int64_t slot, int& b, int& t0, int& r0) {
+    const int G = a.G;
+    auto first = [G](int off, int b) { return (int64_t)off * G / kTileRows + b; };
+    b = seq_of_slot(c, slot, first);
+    int n;
+    seq_rows(c, b, t0, n);
+    const int64_t R = (int64_t)n * G, r = (slot - first(t0, b)) * kTileRows;
+    r0 = (int)r;
+    return R <= a.few || r >= R ? 0 : (int)min(R - r, (int64_t)kTileRows);
+}
+
+template <int D, bool FP8, bool F16>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tile_kernel(KvView c, AttnArgs a, int64_t n_slots,
+                                                                        int32_t splits) {
+    constexpr int ND = D / 64, NK = D / 16, NV = D / 32;
+    __shared__ uint4v lk[2][2][NK][64];      // keys: [buffer][32 tokens][16 dimensions][lane]
+    __shared__ uint4v lv[2][4][NV][64];      // values: [buffer][16 tokens][32 dimensions][lane]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 31, hi = lane >> 5;
+    const int h = blockIdx.x % c.H;
+    const int sp = (int)((blockIdx.x / c.H) % splits);
+    const int64_t slot = n_slots - 1 - blockIdx.x / c.H / splits;     // a sequence's last rows see most: first
+    int b, t0, r0;
+    const int rows = tile_of_slot(c, a, slot, b, t0, r0);
+    if (rows == 0) return;
+    const int64_t past = max(c.past[b], 0);
+    const TileWork work = tile_work(c, a, past, r0, rows, sp, splits);
+    const Span span = work.span;
+    if (sp >= work.shares) return;
+    int n_all, t_;
+    seq_rows(c, b, t_, n_all);
+    const int64_t end_tok = min(past + n_all, (int64_t)c.W << c.page_shift);
+
+    // this wave's rows and the positions they span
+    const int w0 = wave * 32, wrows = min(max(rows - w0, 0), 32);
+    const int row = r0 + w0 + col;
+    const int64_t pos = past + row / a.G;
+    const int64_t pos_min = past + (r0 + w0) / a.G, pos_max = past + (r0 + w0 + max(wrows, 1) - 1) / a.G;
+
+    half8 q[NK];
+    float s2 = fabsf(a.scale2);
+    {
+        uint4v raw[NK];
+        const uint16_t* p = a.q + (int64_t)(t0 + row / a.G) * a.q_stride + ((int64_t)h * a.G + row % a.G) * D + hi * 8;
+        const uint32_t flip = a.scale2 < 0.0f ? 0x80008000u : 0u;
+#pragma unroll
+        for (int s = 0; s < NK; ++s)
+            raw[s] = (col < wrows ? *reinterpret_cast<const uint4v*>(p + s * 16) : uint4v{0, 0, 0, 0}) ^ flip;
+        if constexpr (F16) {
+#pragma unroll
+            for (int s = 0; s < NK; ++s) q[s] = __builtin_bit_cast(half8, raw[s]);
+        } else {
+            uint32_t top = 0;
+#pragma unroll
+            for (int s = 0; s < NK; ++s)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    top = max(top, max((raw[s][i] << 16) & 0x7FFFFFFFu, raw[s][i] & 0x7FFF0000u));
+            top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+            const float f = half_range_factor(top);
+#pragma unroll
+            for (int s = 0; s < NK; ++s)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2v x = unpack2<false>(raw[s][i]);
+                    q[s][2 * i] = (_Float16)(x.x * f);
+                    q[s][2 * i + 1] = (_Float16)(x.y * f);
                 }
-            x = acc * c.ks[page * c.H + h] * scale;
-            vs = c.vs[page * c.H + h];
-        }
-        const float m2 = fmaxf(m, wave_max(x));
-        const float f = m == -INFINITY ? 0.0f : expf(m - m2);
-        const float p = page >= 0 ? expf(x - m2) : 0.0f;
-        m = m2;
-        float s = p;
-        for (int k = 32; k >= 1; k >>= 1) s += __shfl_xor(s, k);
-        l = l * f + s;
-        for (int i = 0; i < nd; ++i) o[i] *= f;
-        for (int k = 0; k < 64; ++k) {
-            const int pk = __shfl((int)page, k);
-            if (pk < 0) continue;
-            const float pv = __shfl(p * vs, k);
-            const int rk = (int)(j0 + k) & (c.page - 1);
-            const uint8_t* tv = c.v + block_at(c, pk, h, rk >> 4) + ((rk & 15) >> 2) * 256 + lane * 4 + (rk & 3);
-            for (int i = 0; i < nd; ++i) o[i] = fmaf(pv, code_values<FP8>(tv[i * 1024]).x, o[i]);
+            s2 *= half_range_undo(top);
         }
     }
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-    for (int i = 0; i < nd; ++i)
-        out[t * out_stride + (int64_t)hq * c.D + i * 64 + lane] = (uint16_t)pack2<F16>(o[i] * inv, 0.0f);
+    s2 = fmaxf(s2, 1e-30f);          // a hidden token's score stays -inf under it
+
+    struct Meta { int32_t page[4]; float ks[4], vs[4]; };
+    auto find_pages = [&](int t, Meta& m) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = t * 4 + e;
+            int32_t p = -1;
+            if (t < work.u1 && i < span.n) {
+                p = uniform_load(c.pages + (int64_t)b * c.W + (span.tile(i) >> (c.page_shift - 4)));
+                if (p >= c.n_pages) p = -1;
+            }
+            m.page[e] = p;
+        }
+    };
+    auto find_scales = [&](Meta& m) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            m.ks[e] = m.vs[e] = 1.0f;
+            if (m.page[e] >= 0) {
+                m.ks[e] = uniform_load(c.ks + (int64_t)m.page[e] * c.H + h);
+                m.vs[e] = uniform_load(c.vs + (int64_t)m.page[e] * c.H + h);
+            }
+        }
+    };
+    // the wave's share of a step: block `wave` of the four
+    uint4v rk[ND], rv[ND];
+    auto fetch = [&](int t, const Meta& m) {
+        const int32_t page = wave == 0 ? m.page[0] : wave == 1 ? m.page[1] : wave == 2 ? m.page[2] : m.page[3];
+        const int32_t blk = span.tile(t * 4 + wave);
+        const int64_t base = page < 0 ? 0 : block_at(c, page, h, blk & ((c.page >> 4) - 1));
+        const uint8_t* kp = c.k + base + (lane & 15) * 64 + (lane >> 4) * 16;
+        const uint8_t* vp = c.v + base + lane * 16;
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) {
+            rk[dt] = *reinterpret_cast<const uint4v*>(kp + dt * 1024);
+            rv[dt] = *reinterpret_cast<const uint4v*>(vp + dt * 1024);
+        }
+        // codes of nobody's tokens may be NaN: out of the product
+        const int64_t tok = (int64_t)blk * 16 + (lane >> 4) * 4;
+        if (page < 0 || (int64_t)blk * 16 + 16 > end_tok) {
+            const int64_t left = page >= 0 ? end_tok - tok : 0;
+            const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * (int)left)) - 1;
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) rv[dt] &= keep;
+        }
+    };
+    auto stage = [&](int buf) {
+        // keys: lane (token lane % 16, dimensions 16 (lane / 16) ..) holds both halves of a product step's operand
+        const int kl = (wave & 1) * 16 + (lane & 15);
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) {
+            uint4v* d = lk[buf][wave >> 1][dt * 4 + (lane >> 4)];
+            d[kl] = __builtin_bit_cast(uint4v, code_halves8<FP8>(rk[dt][0], rk[dt][1]));
+            d[32 + kl] = __builtin_bit_cast(uint4v, code_halves8<FP8>(rk[dt][2], rk[dt][3]));
+        }
+        // values: lanes 32 apart hold token groups g and g + 2 of four dimensions; after the exchange each holds both
+        // groups of two dimensions, one operand register set each
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) {
+            const auto x = __builtin_amdgcn_permlane32_swap(rv[dt][0], rv[dt][2], false, false);
+            const auto y = __builtin_amdgcn_permlane32_swap(rv[dt][1], rv[dt][3], false, false);
+            uint4v* d = &lv[buf][wave][dt * 2 + hi][((lane >> 4) & 1) * 32 + (lane & 15)];
+            d[0] = __builtin_bit_cast(uint4v, code_halves8<FP8>(x[0], x[1]));
+            d[16] = __builtin_bit_cast(uint4v, code_halves8<FP8>(y[0], y[1]));
+        }
+    };
+
+    float m_run = kNoMax, l_run = 0.0f;
+    float16v o[NV] = {};
+    auto compute = [&](int t, int buf, const Meta& m) {
+        bool any = false, full[4];
+        int64_t tok[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            tok[e] = (int64_t)span.tile(t * 4 + e) * 16;
+            any |= m.page[e] >= 0 && tok[e] <= pos_max &&
+                   (a.window == 0 || tok[e] + 15 > pos_min - a.window || tok[e] < a.sinks);
+            full[e] = m.page[e] >= 0 && tok[e] + 15 <= pos_min &&
+                      (a.window == 0 || tok[e] > pos_max - a.window || tok[e] + 15 < a.sinks);
+        }
+        if (wrows == 0 || !any) return;
+        float16v s[2] = {};
+#pragma unroll
+        for (int k = 0; k < NK; ++k)
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+                s[g] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, lk[buf][g][k][lane]), q[k], s[g],
+                                                              0, 0, 0);
+        float f[4], lg[4], mx = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (!full[e]) {
+                const Sight v = sight(a, m.page[e], pos, tok[e]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float x = s[e >> 1][(e & 1) * 8 + i];
+                    s[e >> 1][(e & 1) * 8 + i] = v.sees(8 * (i >> 2) + 4 * hi + (i & 3)) ? x : -INFINITY;
+                }
+            }
+            f[e] = m.ks[e] * s2;
+            lg[e] = __builtin_amdgcn_logf(m.vs[e]);
+            float top = s[e >> 1][(e & 1) * 8];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) top = fmaxf(top, s[e >> 1][(e & 1) * 8 + i]);
+            mx = fmaxf(mx, fmaf(top, f[e], lg[e]));
+        }
+        if (__any(mx > m_run + kGrow)) {
+            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            const float m2 = fmaxf(m_run, mx);
+            const float r = __builtin_amdgcn_exp2f(m_run - m2);
+            m_run = m2;
+            l_run *= r;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) o[i] *= r;
+        }
+        half8 p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float off = lg[e] - (m_run - kTop);
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float w = __builtin_amdgcn_exp2f(fmaf(s[e >> 1][(e & 1) * 8 + i], f[e], off));
+                sum += w;
+                p[e][i] = (_Float16)w;
+            }
+            l_run = fmaf(sum, __builtin_amdgcn_rcpf(m.vs[e]), l_run);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, lv[buf][e][i][lane]), p[e], o[i],
+                                                              0, 0, 0);
+    };
+
+    // pages are looked up three steps ahead, codes fetched two and scales one
+    Meta m0, m1, m2, m3;
+    find_pages(work.u0, m0);
+    find_pages(work.u0 + 1, m1);
+    find_pages(work.u0 + 2, m2);
+    find_scales(m0);
+    fetch(work.u0, m0);
+    stage(work.u0 & 1);
+    fetch(work.u0 + 1, m1);
+    __syncthreads();
+    for (int t = work.u0; t < work.u1; ++t) {
+        // the other buffer's readers passed the barrier that ended the step before
+        stage((t + 1) & 1);
+        find_pages(t + 3, m3);
+        find_scales(m1);
+        fetch(t + 2, m2);
+        compute(t, t & 1, m0);
+        __syncthreads();
+        m0 = m1;
+        m1 = m2;
+        m2 = m3;
+    }
+
+    l_run += __shfl_xor(l_run, 32);
+    if (col >= wrows) return;
+    if (work.shares == 1) {
+        const float norm = l_run > 0.0f ? 1.0f / l_run : 0.0f;
+        uint16_t* out = a.out + (int64_t)(t0 + row / a.G) * a.out_stride + ((int64_t)h * a.G + row % a.G) * D;
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                uint32_t w[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        w[2 * i + e] = pack2<F16>(o[dt * 2 + e][4 * k + i] * norm, o[dt * 2 + e][8 + 4 * k + i] * norm);
+                uint4v* d = reinterpret_cast<uint4v*>(out + dt * 64 + k * 32 + hi * 16);
+                d[0] = uint4v{w[0], w[1], w[2], w[3]};
+                d[1] = uint4v{w[4], w[5], w[6], w[7]};
+            }
+    } else {
+        const int64_t at = (((slot * c.H + h) * splits + sp) * kTileRows + w0 + col);
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    *reinterpret_cast<float4v*>(a.part_o + at * D + dt * 64 + k * 32 + hi * 16 + i * 4) =
+                        float4v{o[dt * 2][4 * k + i], o[dt * 2][8 + 4 * k + i], o[dt * 2 + 1][4 * k + i],
+                                o[dt * 2 + 1][8 + 4 * k + i]};
+        if (hi == 0) a.part_ml[at] = float2v{m_run, l_run};
+    }
+}
+
+// Adds the partial sums of a tile's shares in their order: a workgroup for each
+// eight rows of a tile and kv head.
+template <int D, bool F16>
+__global__ __launch_bounds__(256) void kv_tile_join_kernel(KvView c, AttnArgs a, int32_t splits) {
+    constexpr int kPieces = kTileRows / 8;
+    const int piece = blockIdx.x % kPieces, h = (blockIdx.x / kPieces) % c.H;
+    const int64_t slot = blockIdx.x / kPieces / c.H;
+    int b, t0, r0;
+    const int rows = tile_of_slot(c, a, slot, b, t0, r0);
+    const int i = piece * 8 + (threadIdx.x >> 5), d0 = (threadIdx.x & 31) * (D / 32);
+    if (i >= rows) return;
+    const int shares = tile_work(c, a, max(c.past[b], 0), r0, rows, 0, splits).shares;
+    if (shares == 1) return;
+    float m = kNoMax, l = 0.0f, v[D / 32] = {};
+    for (int sp = 0; sp < shares; ++sp) {
+        const int64_t at = ((slot * c.H + h) * splits + sp) * kTileRows + i;
+        const float2v p = a.part_ml[at];
+        const float m2 = fmaxf(m, p.x);
+        const float f = __builtin_amdgcn_exp2f(m - m2), e = __builtin_amdgcn_exp2f(p.x - m2);
+        m = m2;
+        l = l * f + p.y * e;
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) v[k] = v[k] * f + a.part_o[at * D + d0 + k] * e;
+    }
+    const float norm = l > 0.0f ? 1.0f / l : 0.0f;
+    const int row = r0 + i;
+    uint16_t* out = a.out + (int64_t)(t0 + row / a.G) * a.out_stride + ((int64_t)h * a.G + row % a.G) * D + d0;
+#pragma unroll
+    for (int k = 0; k < D / 32; k += 2) *reinterpret_cast<uint32_t*>(out + k) = pack2<F16>(v[k] * norm, v[k + 1] * norm);
+}
+
+// Shares of a tile: enough workgroups for two on every compute unit, where the workspace holds their sums.
+int tile_splits(const KvView& c, int64_t slots, int n_cu, int64_t room) {
+    const int64_t tiles = slots * c.H, one = tiles * kTileRows * (c.D + 2) * 4;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({(2 * (int64_t)n_cu + tiles - 1) / tiles, room / one, 64}));
 }
 
 }  // namespace
 
-int64_t kv_attention_workspace_bytes(const KvView& c, int n_cu) {
-    const int64_t slots = (int64_t)n_cu * 2 * 2 * 16;
-    return slots * (c.D + 2) * 4 + ((int64_t)c.B + 2) * 8;
-}
-
 hipError_t launch_kv_attention(const KvView& c, const void* q, int64_t q_stride, int32_t Hq, float scale,
-                               int32_t window, int32_t sinks, void* out, int64_t out_stride, void* workspace, int n_cu,
-                               hipStream_t s) {
-    const int64_t groups = ((int64_t)c.T * Hq + 3) / 4;
-    if (groups >= (int64_t)1 << 24 || (int64_t)c.B * c.H >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
+                               int32_t window, int32_t sinks, void* out, int64_t out_stride, void* workspace,
+                               int64_t workspace_bytes, int n_cu, hipStream_t s) {
     AttnArgs a;
     a.q = (const uint16_t*)q;
     a.out = (uint16_t*)out;
@@ -494,28 +779,42 @@ hipError_t launch_kv_attention(const KvView& c, const void* q, int64_t q_stride,
     a.scale2 = scale * 1.4426950408889634f;
     a.window = window;
     a.sinks = sinks;
-    a.few = 16;
-    const uint32_t wgs = (uint32_t)n_cu * 2;
-    const int64_t slots = (int64_t)wgs * 2 * 16;
-    a.first = (int64_t*)workspace;
-    a.part_ml = (float2v*)(a.first + c.B + 2);
-    a.part_o = (float*)(a.part_ml + slots) + (c.B & 1 ? 2 : 0);       // 16-byte aligned
-    hipError_t e = by_types(c, [&](auto fp8, auto f16) {
+    a.few = kFewRows;
+    // the split kernel's workspace, then the tiles' (they may run one after the other on the same memory)
+    const int64_t wgs = (int64_t)n_cu * 2, split_rows = wgs * 2 * kFewRows;
+    WsCarve ws{(char*)workspace, (size_t)workspace_bytes};
+    a.first = ws.take<int64_t>((int64_t)c.B + 2);
+    const size_t head = ws.off;
+    a.part_ml = ws.take<float2v>(split_rows);
+    a.part_o = ws.take<float>(split_rows * c.D);
+    const int64_t slots = (int64_t)c.T * a.G / kTileRows + c.B;
+    if (!ws.ok() || (int64_t)c.B * c.H >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
+    const bool tiles = (int64_t)c.max_new * a.G > a.few;
+    const int splits = tiles ? tile_splits(c, slots, n_cu, workspace_bytes - (int64_t)head - 4096) : 1;
+    if (tiles && slots * c.H * std::max(splits, kTileRows / 8) >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
+    return by_types(c, [&](auto fp8, auto f16) {
         auto run = [&](auto d) {
             constexpr int D = decltype(d)::value;
-            kv_split_kernel<D, fp8.value, f16.value><<<wgs, 256, 0, s>>>(c, a, 2);
+            kv_split_kernel<D, fp8.value, f16.value><<<(uint32_t)wgs, 256, 0, s>>>(c, a, 2);
             kv_join_kernel<D, f16.value><<<(uint32_t)(c.B * c.H), 256, 0, s>>>(c, a);
+            if (tiles) {
+                AttnArgs t = a;
+                WsCarve w{(char*)workspace, (size_t)workspace_bytes, head};
+                if (splits > 1) {
+                    t.part_ml = w.take<float2v>(slots * c.H * splits * kTileRows);
+                    t.part_o = w.take<float>(slots * c.H * splits * kTileRows * D);
+                }
+                kv_tile_kernel<D, fp8.value, f16.value>
+                    <<<(uint32_t)(slots * c.H * splits), 256, 0, s>>>(c, t, slots, splits);
+                if (splits > 1)
+                    kv_tile_join_kernel<D, f16.value>
+                        <<<(uint32_t)(slots * c.H * (kTileRows / 8)), 256, 0, s>>>(c, t, splits);
+            }
             return hipGetLastError();
         };
         if (c.D == 64) return run(std::integral_constant<int, 64>{});
         if (c.D == 128) return run(std::integral_constant<int, 128>{});
         return run(std::integral_constant<int, 256>{});
-    });
-    if (e != hipSuccess || (int64_t)c.max_new * a.G <= a.few) return e;
-    return by_types(c, [&](auto fp8, auto f16) {
-        kv_attend_kernel<fp8.value, f16.value><<<(uint32_t)groups, 256, 0, s>>>(
-            c, (const uint16_t*)q, q_stride, Hq, scale, window, sinks, (uint16_t*)out, out_stride, a.few);
-        return hipGetLastError();
     });
 }
 

@@ -1483,12 +1483,10 @@ int ls_kv_attention(ls_ctx* c, const ls_kv_cache* cache, const ls_kv_batch* batc
     DeviceScope dev(c->device);
     if (!dev.ok) return fail(c, LS_ERR_DEVICE, "cannot select device %d", c->device);
     hipStream_t s = (hipStream_t)stream;
-    if (ls::kv_attention_workspace_bytes(w, c->n_cu_dev) > LS_KV_WORKSPACE_BYTES)
-        return fail(c, LS_ERR_UNSUPPORTED, "the batch is too large for the workspace");
     if ((rc = grow(c, &c->kv_ws, &c->kv_ws_cap, LS_KV_WORKSPACE_BYTES, s))) return rc;
     Timed t(c, K_KV_ATTENTION, s);
     const hipError_t e = ls::launch_kv_attention(w, q, q_stride, n_q_heads, scale, window, sinks, out, out_stride,
-                                                 c->kv_ws, c->n_cu, s);
+                                                 c->kv_ws, (int64_t)c->kv_ws_cap, c->n_cu, s);
     t.done();
     return kv_launched(c, e);
 }
