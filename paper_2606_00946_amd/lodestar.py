@@ -282,6 +282,14 @@ def _rows(t, name, batch, D, heads=None, like=None):
     return t.data_ptr(), s[0] if n > 1 else h * D, h
 
 
+def _raw_stream(stream, device):
+    """The HIP stream of a call: the given one, or the context's device's current one."""
+    if stream is None:
+        import torch
+        return torch._C._cuda_getCurrentRawStream(device)
+    return stream.cuda_stream
+
+
 class Context:
     """One ls_ctx: model, cache state and workspace on one device."""
 
@@ -555,7 +563,7 @@ class Context:
             op, os_, _ = _rows(q_out, "q_out", batch, D, qh, k)
         return self._check("ls_kv_append",
                            self.lib.ls_kv_append(self.h, cache.ref, batch.ref, None if rope is None else rope.ref,
-                                                 kp, ks, vp, vs, qp, qs, qh, op, os_, _stream(stream)))
+                                                 kp, ks, vp, vs, qp, qs, qh, op, os_, _raw_stream(stream, self.device)))
 
     def ls_kv_attention(self, cache, batch, q, out, scale=None, window=0, sinks=0, stream=None):
         """out [T x q heads x D]: attention of the batch's rows over the cache; scale defaults to 1 / sqrt(D)."""
@@ -565,7 +573,7 @@ class Context:
         return self._check("ls_kv_attention",
                            self.lib.ls_kv_attention(self.h, cache.ref, batch.ref, qp, qs, qh,
                                                     D ** -0.5 if scale is None else scale, window, sinks, op, os_,
-                                                    _stream(stream)))
+                                                    _raw_stream(stream, self.device)))
 
     def ls_kv_read(self, cache, batch, k_out, v_out, stream=None):
         """The keys and values [T x kv heads x D] that the cache holds for the batch's tokens."""
@@ -575,7 +583,7 @@ class Context:
                 raise ValueError(f"{name} must be contiguous")
         kp, _, _ = _rows(k_out, "k_out", batch, D, H)
         vp, _, _ = _rows(v_out, "v_out", batch, D, H, k_out)
-        return self._check("ls_kv_read", self.lib.ls_kv_read(self.h, cache.ref, batch.ref, kp, vp, _stream(stream)))
+        return self._check("ls_kv_read", self.lib.ls_kv_read(self.h, cache.ref, batch.ref, kp, vp, _raw_stream(stream, self.device)))
 
     # -- per-kernel timing ------------------------------------------------
     def ls_profile_enable(self, enable=True):
