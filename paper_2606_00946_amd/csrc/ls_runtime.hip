@@ -1461,7 +1461,8 @@ int ls_kv_append(ls_ctx* c, const ls_kv_cache* cache, const ls_kv_batch* batch, 
     hipStream_t s = (hipStream_t)stream;
     Timed t(c, K_KV_APPEND, s);
     const hipError_t e =
-        ls::launch_kv_append(w, r, k, k_stride, v, v_stride, q, q_stride, n_q_heads, q_out, q_out_stride, s);
+        ls::launch_kv_append(w, r, k, k_stride, v, v_stride, q, q_stride, n_q_heads, q_out, q_out_stride,
+                             c->n_cu, s);
     t.done();
     return kv_launched(c, e);
 }
