@@ -19,8 +19,6 @@
 namespace ls {
 namespace {
 
-using mask_t = uint64_t;
-
 struct AttnArgs {
     const uint16_t* q;
     uint16_t* out;
@@ -29,10 +27,10 @@ struct AttnArgs {
     float scale2;                    // softmax scale * log2 e
     int32_t window, sinks;
     int32_t few;                     // sequences with up to this many rows (new tokens x G) split along the keys
-    // joining of split rows: partial sums of each workgroup's first and last segment
-    float* part_o;                   // [workgroups][2][16][D]
-    float2v* part_ml;                // [workgroups][2][16] running maximum and sum
-    int64_t* first;                  // [B + 1] unit of each sequence's start, then the units of a workgroup
+    // segments (sequence, kv head) that are cut: sums of each part, and counts of those that are there
+    float* part_o;                   // [parts][16][D]
+    float2v* part_ml;                // [parts][16] running maximum and sum
+    uint32_t* arrived;               // [parts][2], zero between launches
 };
 
 // What a sequence's rows see, in 16-token blocks: the first n_sink and those from
@@ -71,18 +69,29 @@ __device__ __forceinline__ Sight sight(const AttnArgs& a, int32_t page, int64_t 
 }
 
 constexpr int kFewRows = 16;         // rows of a kv head that kv_split_kernel takes
+constexpr int kMaxParts = 8192;        // of a launch of kv_split_kernel that cuts segments
 constexpr int kUnit = 8;             // 16-token blocks of a work unit: two for each wave of a workgroup
+constexpr int kJoin = 16;            // parts that one workgroup adds
+// Workgroups of kv_split_kernel on a compute unit, by its registers.
+template <int D>
+constexpr int kSplitPerCu = D == 64 ? 4 : D == 128 ? 3 : 1;
+constexpr int kMinUnits = 8;        // no segment is cut finer
 constexpr float kNoMax = -1e30f;     // running maximum of nothing
 constexpr float kTop = 7.0f;         // weights start below 2^7 ...
 constexpr float kGrow = 8.0f;        // ... and the maximum moves when one would pass 2^15
 
-// Units of one kv head of sequence b; 0: not this kernel's.
-__device__ __forceinline__ int32_t units_of(const KvView& c, const AttnArgs& a, int b) {
-    int t0, n;
-    seq_rows(c, b, t0, n);
-    if (n == 0 || (int64_t)n * a.G > a.few) return 0;
-    const Span s = span_of(c, a, max(c.past[b], 0), n);
-    return max((s.n + kUnit - 1) / kUnit, 1);
+// A sequence of the call as kv_split_kernel sees it; units of one kv head, 0: not that kernel's.
+struct Seq {
+    int32_t t0, n, past, units;
+};
+__device__ __forceinline__ Seq seq_of(const KvView& c, const AttnArgs& a, int b) {
+    Seq s;
+    seq_rows(c, b, s.t0, s.n);
+    s.past = max(c.past[b], 0);
+    s.units = 0;
+    if (s.n != 0 && (int64_t)s.n * a.G <= a.few)
+        s.units = max((span_of(c, a, s.past, s.n).n + kUnit - 1) / kUnit, 1);
+    return s;
 }
 
 // Power of two that brings a row of bf16 queries whose largest magnitude has the
@@ -141,77 +150,169 @@ __device__ __forceinline__ float load_queries(const AttnArgs& a, int D_heads_h, 
     }
 }
 
-// Few rows (up to 16 of a kv head) against a long cache: bound by HBM.  All the
-// sequences' heads are laid end to end in units of 128 tokens and cut into equal
-// shares, one workgroup each, whatever the lengths; a segment (sequence, head)
-// that lies in one share is finished there, the others leave partial sums that
-// kv_join_kernel adds.  A wave takes 32 of a unit's tokens at a time: scores
-// transposed (tokens x rows), so that their registers are the second operand of
-// the product with the values as they stand; codes go from memory to registers in
-// 16-byte loads, one step ahead of their use.
+// Two floats to, and from, memory that other workgroups of the launch read and
+// write: past the caches that each XCD has for itself.  A fence would write back and
+// drop that whole cache instead, in every workgroup: twice the kernel's time.
+__device__ __forceinline__ void put_shared(float* p, float2v x) {
+    __hip_atomic_store((uint64_t*)p, __builtin_bit_cast(uint64_t, x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2v get_shared(const float* p) {
+    return __builtin_bit_cast(float2v, __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+
+// Partial sums of a segment's 16 rows: a thread holds dimensions d0 .. d0 + 3 of
+// every 64 of a row.
+template <int D>
+__device__ __forceinline__ void put_part(const AttnArgs& a, int64_t part, int row, int d0, int rows,
+                                         const float4v (&v)[D / 64], float m, float l) {
+    if (row >= rows) return;
+    const int64_t at = part * kFewRows + row;
+#pragma unroll
+    for (int dt = 0; dt < D / 64; ++dt) {
+        put_shared(a.part_o + at * D + dt * 64 + d0, float2v{v[dt].x, v[dt].y});
+        put_shared(a.part_o + at * D + dt * 64 + d0 + 2, float2v{v[dt].z, v[dt].w});
+    }
+    if (d0 == 0) put_shared((float*)&a.part_ml[at], float2v{m, l});
+}
+
+// Counts the workgroup's part as written; whether it was the last of `members`,
+// whose parts are then all to be read here.  Nobody waits.  The last one leaves the
+// count at zero for the next launch.
+__device__ __forceinline__ bool arrive(uint32_t* count, int members) {
+    __shared__ int is_last;
+    // every thread's stores are past the caches before any of them passes the barrier
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const uint32_t before = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        is_last = before == (uint32_t)members - 1;
+        if (is_last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    return is_last;
+}
+
+// Adds n parts, `step` apart from `first`, in their order; eight are read at a time.
+template <int D>
+__device__ __forceinline__ void add_parts(const AttnArgs& a, uint32_t first, int step, int n, int row, int d0, int rows,
+                                          float4v (&v)[D / 64], float& m, float& l) {
+    constexpr int kAtOnce = D == 256 ? 4 : 8;
+    if (row >= rows) return;
+    m = kNoMax;
+    l = 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < D / 64; ++dt) v[dt] = float4v{0, 0, 0, 0};
+    for (int i0 = 0; i0 < n; i0 += kAtOnce) {
+        float2v ml[kAtOnce], x[kAtOnce][D / 64][2];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int64_t at = ((int64_t)first + (int64_t)min(i0 + i, n - 1) * step) * kFewRows + row;
+            ml[i] = get_shared((const float*)&a.part_ml[at]);
+#pragma unroll
+            for (int dt = 0; dt < D / 64; ++dt) {
+                x[i][dt][0] = get_shared(a.part_o + at * D + dt * 64 + d0);
+                x[i][dt][1] = get_shared(a.part_o + at * D + dt * 64 + d0 + 2);
+            }
+        }
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) top = fmaxf(top, ml[i].x);
+        const float f = __builtin_amdgcn_exp2f(m - top);
+        m = top;
+        l *= f;
+#pragma unroll
+        for (int dt = 0; dt < D / 64; ++dt) v[dt] *= f;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const float e = i0 + i < n ? __builtin_amdgcn_exp2f(ml[i].x - m) : 0.0f;
+            l = fmaf(ml[i].y, e, l);
+#pragma unroll
+            for (int dt = 0; dt < D / 64; ++dt)
+                v[dt] += float4v{x[i][dt][0].x, x[i][dt][0].y, x[i][dt][1].x, x[i][dt][1].y} * e;
+        }
+    }
+}
+
+// Few rows (up to 16 of a kv head) against a long cache: bound by HBM.  The
+// sequences' heads are cut into parts of about equal length, a workgroup each; a
+// segment (sequence, head) of one part is finished there, the others leave partial
+// sums, which the last workgroup to finish adds.  A wave takes 32 of a unit's 128
+// tokens at a time: scores transposed (tokens x rows), so that their registers are
+// the second operand of the product with the values as they stand; codes go from
+// memory to registers in 16-byte loads, one step ahead of their use.
 template <int D, bool FP8, bool F16>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_split_kernel(KvView c, AttnArgs a, int32_t min_units) {
+__global__ __launch_bounds__(256, kSplitPerCu<D>) void kv_split_kernel(KvView c, AttnArgs a, bool cut) {
     constexpr int ND = D / 64;
     __shared__ float comb[4][16][D + 4];
     __shared__ float2v ml[4][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
 
-    // the launch's units, this workgroup's share and where it starts
-    int64_t total = 0;
-    for (int b = lane; b < c.B; b += 64) total += units_of(c, a, b);
+    // Segments are cut into equal parts of at most `most` units, so that about gridDim.x parts hold all units and a
+    // long sequence weighs no more on one workgroup than its share (not cut: a part is a segment, found at once).
+    uint32_t most = ~0u;
+    if (cut) {
+        uint64_t total = 0;
+        for (int b = lane; b < c.B; b += 64) total += seq_of(c, a, b).units;
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o);
-    total = uniform(total) * c.H;
-    const int64_t share = max((total + gridDim.x - 1) / gridDim.x, (int64_t)min_units);
-    int64_t at = (int64_t)blockIdx.x * share;
-    const int64_t stop = min(at + share, total);
-    const bool scribe = blockIdx.x == 0 && wave == 0;        // writes the sequences' starts for the join
-    if (at >= stop && !scribe) return;
-    int b = 0;
-    int64_t start = 0;               // first unit of sequence b
-    {
-        int64_t base = 0;
-        bool found = false;
-        for (int b0 = 0; b0 < c.B; b0 += 64) {
-            const int64_t u = b0 + lane < c.B ? (int64_t)units_of(c, a, b0 + lane) * c.H : 0;
-            int64_t end = u;         // inclusive sums
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int64_t v = __shfl_up(end, o);
-                if (lane >= o) end += v;
-            }
-            end += base;
-            if (scribe && b0 + lane < c.B) a.first[b0 + lane] = end - u;
-            const mask_t m = __ballot(end > at);
-            if (!found && m) {
-                const int k = __ffsll((long long)m) - 1;
-                b = b0 + k;
-                start = __shfl(end - u, k);
-                found = true;
-                if (!scribe) break;
-            }
-            base = __shfl(end, 63);
-        }
-        if (scribe && lane == 0) {
-            a.first[c.B] = total;
-            a.first[c.B + 1] = share;
-        }
+        for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o);
+        const uint64_t all = (uint64_t)uniform((int64_t)total) * c.H;
+        const uint32_t room = gridDim.x - (uint32_t)(c.B * c.H);
+        // 2^24 units and more, the largest segment, cut nothing
+        const uint64_t each = all >> 31 ? (all + room - 1) / room : ((uint32_t)all + room - 1) / room;
+        most = (uint32_t)min(max(each, (uint64_t)kMinUnits), (uint64_t)1 << 24);
     }
-    b = __builtin_amdgcn_readfirstlane(b);
-    start = uniform(start);
-
-    while (at < stop) {
-        const int32_t per_head = units_of(c, a, b);
-        if (per_head == 0) { ++b; continue; }
-        int t0, n;
-        seq_rows(c, b, t0, n);
-        const int64_t past = max(c.past[b], 0);
+    for (uint32_t part = blockIdx.x;; part += gridDim.x) {
+        Seq seq;
+        int b = 0, h, piece = 0, pieces = 1;
+        uint32_t seg = part;             // first part of the segment
+        if (cut) {
+            // sequences' first parts are the sums of the parts before them
+            uint32_t base = 0;
+            int b0 = 0;
+            Seq mine;
+            uint64_t m = 0;
+            uint32_t own = 0, end = 0;
+            for (; b0 < c.B; b0 += 64) {
+                mine.units = 0;
+                if (b0 + lane < c.B) mine = seq_of(c, a, b0 + lane);
+                own = ((uint32_t)mine.units + most - 1) / most;
+                end = own * (uint32_t)c.H;           // inclusive sums
+#pragma unroll
+                for (int o = 1; o < 64; o <<= 1) {
+                    const uint32_t v = __shfl_up(end, o);
+                    if (lane >= o) end += v;
+                }
+                end += base;
+                m = __ballot(end > part);
+                if (m) break;
+                base = __builtin_amdgcn_readlane(end, 63);
+            }
+            if (!m) return;
+            const int k = __ffsll((long long)m) - 1;
+            b = b0 + k;
+            seq.t0 = __builtin_amdgcn_readlane(mine.t0, k);
+            seq.n = __builtin_amdgcn_readlane(mine.n, k);
+            seq.past = __builtin_amdgcn_readlane(mine.past, k);
+            seq.units = __builtin_amdgcn_readlane(mine.units, k);
+            pieces = __builtin_amdgcn_readlane(own, k);
+            const uint32_t start = __builtin_amdgcn_readlane(end, k) - (uint32_t)pieces * c.H;
+            h = (int)((part - start) / (uint32_t)pieces);
+            seg = start + (uint32_t)h * pieces;
+            piece = (int)(part - seg);
+        } else {
+            if (part >= (uint32_t)(c.B * c.H)) return;
+            b = (int)(part / (uint32_t)c.H);
+            h = (int)(part % (uint32_t)c.H);
+            seq = seq_of(c, a, b);
+            if (seq.units == 0) continue;
+        }
+        const int t0 = seq.t0, n = seq.n;
+        const int64_t past = seq.past;
         const Span span = span_of(c, a, past, n);
         const int64_t end_tok = min(past + n, (int64_t)c.W << c.page_shift);
-        const int32_t h = (int32_t)((at - start) / per_head);
-        const int32_t u0 = (int32_t)((at - start) - (int64_t)h * per_head);
-        const int32_t u1 = (int32_t)min((int64_t)per_head, u0 + (stop - at));
+        const int32_t u0 = (int32_t)((int64_t)seq.units * piece / pieces);
+        const int32_t u1 = (int32_t)((int64_t)seq.units * (piece + 1) / pieces);
         const int rows = n * a.G;
         const int64_t pos = past + col / a.G;                // the column's position
         const int64_t pos_last = past + n - 1;
@@ -366,70 +467,43 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_split_kernel(KvView 
         for (int w = 0; w < 4; ++w) m_row = fmaxf(m_row, ml[w][row].x);
 #pragma unroll
         for (int w = 0; w < 4; ++w) l_row = fmaf(ml[w][row].y, __builtin_amdgcn_exp2f(ml[w][row].x - m_row), l_row);
-        const bool whole = u0 == 0 && u1 == per_head;
-        const float norm = l_row > 0.0f ? 1.0f / l_row : 0.0f;
-        const int64_t slot = ((int64_t)blockIdx.x * 2 + (u0 == 0 ? 1 : 0)) * 16 + row;
-        if (row < rows) {
-            uint16_t* out = a.out + (int64_t)(t0 + row / a.G) * a.out_stride + ((int64_t)h * a.G + row % a.G) * D;
+        float4v v[ND];
 #pragma unroll
-            for (int dt = 0; dt < ND; ++dt) {
-                float4v v = {0, 0, 0, 0};
+        for (int dt = 0; dt < ND; ++dt) {
+            v[dt] = *reinterpret_cast<const float4v*>(&comb[0][row][dt * 64 + d0]);
 #pragma unroll
-                for (int w = 0; w < 4; ++w) v += *reinterpret_cast<const float4v*>(&comb[w][row][dt * 64 + d0]);
-                if (whole) {
-                    v *= norm;
-                    *reinterpret_cast<uint2v*>(out + dt * 64 + d0) =
-                        uint2v{pack2<F16>(v.x, v.y), pack2<F16>(v.z, v.w)};
-                } else {
-                    *reinterpret_cast<float4v*>(a.part_o + slot * D + dt * 64 + d0) = v;
+            for (int w = 1; w < 4; ++w) v[dt] += *reinterpret_cast<const float4v*>(&comb[w][row][dt * 64 + d0]);
+        }
+        bool last = true;
+        if (pieces > 1) {
+            // Parts are added in groups of kJoin: whoever finishes a group's last part adds the group's parts,
+            // whoever finishes the last group adds the groups' sums; always in the order of the parts.
+            const int gr = piece / kJoin, members = min(kJoin, pieces - gr * kJoin), groups = (pieces - 1) / kJoin + 1;
+            const uint32_t lead = seg + (uint32_t)gr * kJoin;        // the group's first part
+            put_part<D>(a, part, row, d0, rows, v, m_row, l_row);
+            last = arrive(a.arrived + (int64_t)lead * 2, members);
+            if (last) {
+                add_parts<D>(a, lead, 1, members, row, d0, rows, v, m_row, l_row);
+                if (groups > 1) {
+                    // the group's sum in the place of its first part, which all of the workgroup has read
+                    __syncthreads();
+                    put_part<D>(a, lead, row, d0, rows, v, m_row, l_row);
+                    last = arrive(a.arrived + (int64_t)seg * 2 + 1, groups);
+                    if (last) add_parts<D>(a, seg, kJoin, groups, row, d0, rows, v, m_row, l_row);
                 }
             }
-            if (!whole && d0 == 0) a.part_ml[slot] = float2v{m_row, l_row};
+        }
+        if (last && row < rows) {
+            const float norm = l_row > 0.0f ? 1.0f / l_row : 0.0f;
+            uint16_t* out = a.out + (int64_t)(t0 + row / a.G) * a.out_stride + ((int64_t)h * a.G + row % a.G) * D;
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+                *reinterpret_cast<uint2v*>(out + dt * 64 + d0) =
+                    uint2v{pack2<F16>(v[dt].x * norm, v[dt].y * norm), pack2<F16>(v[dt].z * norm, v[dt].w * norm)};
         }
         __syncthreads();
 
-        at += u1 - u0;
-        if (at - start == (int64_t)per_head * c.H) {
-            start = at;
-            ++b;
-        }
     }
-}
-
-// Adds the partial sums of segments that several workgroups shared, in their
-// order.  One workgroup for each sequence and kv head.
-template <int D, bool F16>
-__global__ __launch_bounds__(256) void kv_join_kernel(KvView c, AttnArgs a) {
-    const int b = blockIdx.x / c.H, h = blockIdx.x % c.H;
-    const int64_t share = a.first[c.B + 1];
-    const int64_t s0 = a.first[b], per_head = (a.first[b + 1] - s0) / c.H;
-    if (per_head == 0) return;
-    const int64_t lo = s0 + h * per_head, hi = lo + per_head;
-    const int64_t w0 = lo / share, w1 = (hi - 1) / share;
-    if (w0 == w1) return;
-    int t0, n;
-    seq_rows(c, b, t0, n);
-    const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * 4;
-    if (row >= n * a.G) return;
-    float m = kNoMax, l = 0.0f;
-    float4v v[D / 64] = {};
-    for (int64_t w = w0; w <= w1; ++w) {
-        const int64_t slot = (w * 2 + (w == w0 ? 1 : 0)) * 16 + row;
-        const float2v p = a.part_ml[slot];
-        const float m2 = fmaxf(m, p.x);
-        const float f = __builtin_amdgcn_exp2f(m - m2), e = __builtin_amdgcn_exp2f(p.x - m2);
-        m = m2;
-        l = l * f + p.y * e;
-#pragma unroll
-        for (int dt = 0; dt < D / 64; ++dt)
-            v[dt] = v[dt] * f + *reinterpret_cast<const float4v*>(a.part_o + slot * D + dt * 64 + d0) * e;
-    }
-    const float norm = l > 0.0f ? 1.0f / l : 0.0f;
-    uint16_t* out = a.out + (int64_t)(t0 + row / a.G) * a.out_stride + ((int64_t)h * a.G + row % a.G) * D;
-#pragma unroll
-    for (int dt = 0; dt < D / 64; ++dt)
-        *reinterpret_cast<uint2v*>(out + dt * 64 + d0) =
-            uint2v{pack2<F16>(v[dt].x * norm, v[dt].y * norm), pack2<F16>(v[dt].z * norm, v[dt].w * norm)};
 }
 
 // Many rows (prompts): bound by the matrix cores and the exponentials.  A
@@ -767,6 +841,16 @@ int tile_splits(const KvView& c, int64_t slots, int n_cu, int64_t room) {
 
 }  // namespace
 
+// The counts of a new workspace (kv_split_kernel leaves them at zero).
+__global__ void kv_clear_kernel(uint32_t* p, int n) {
+    for (int i = threadIdx.x; i < n; i += blockDim.x) p[i] = 0;
+}
+
+hipError_t launch_kv_workspace_init(void* workspace, hipStream_t s) {
+    kv_clear_kernel<<<1, 256, 0, s>>>((uint32_t*)workspace, kMaxParts * 2);
+    return hipGetLastError();
+}
+
 hipError_t launch_kv_attention(const KvView& c, const void* q, int64_t q_stride, int32_t Hq, float scale,
                                int32_t window, int32_t sinks, void* out, int64_t out_stride, void* workspace,
                                int64_t workspace_bytes, int n_cu, hipStream_t s) {
@@ -780,23 +864,30 @@ hipError_t launch_kv_attention(const KvView& c, const void* q, int64_t q_stride,
     a.window = window;
     a.sinks = sinks;
     a.few = kFewRows;
-    // the split kernel's workspace, then the tiles' (they may run one after the other on the same memory)
-    const int64_t wgs = (int64_t)n_cu * 2, split_rows = wgs * 2 * kFewRows;
+    // kv_split_kernel's workspace, then the tiles' (they run one after the other on the same memory)
     WsCarve ws{(char*)workspace, (size_t)workspace_bytes};
-    a.first = ws.take<int64_t>((int64_t)c.B + 2);
+    a.arrived = ws.take<uint32_t>(kMaxParts * 2);
     const size_t head = ws.off;
-    a.part_ml = ws.take<float2v>(split_rows);
-    a.part_o = ws.take<float>(split_rows * c.D);
+    // as many parts as workgroups fit the device, and twice the segments where these are more; segments stay whole
+    // where the workspace does not hold that many parts
+    const int64_t segments = (int64_t)c.B * c.H, fit = (int64_t)n_cu * (c.D == 64 ? kSplitPerCu<64> : c.D == 128 ? kSplitPerCu<128> : kSplitPerCu<256>);
+    const int64_t room = std::min<int64_t>((workspace_bytes - (int64_t)head - 4096) / (kFewRows * (c.D + 2) * 4), kMaxParts);
+    const bool cut = segments * 3 <= room * 2;
+    const int64_t wgs = cut ? std::min(std::max(fit, segments * 2), room) : segments;
+    if (wgs >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
+    if (cut) {
+        a.part_ml = ws.take<float2v>(wgs * kFewRows);
+        a.part_o = ws.take<float>(wgs * kFewRows * c.D);
+    }
     const int64_t slots = (int64_t)c.T * a.G / kTileRows + c.B;
-    if (!ws.ok() || (int64_t)c.B * c.H >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
+    if (!ws.ok()) return hipErrorInvalidConfiguration;
     const bool tiles = (int64_t)c.max_new * a.G > a.few;
     const int splits = tiles ? tile_splits(c, slots, n_cu, workspace_bytes - (int64_t)head - 4096) : 1;
     if (tiles && slots * c.H * std::max(splits, kTileRows / 8) >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
     return by_types(c, [&](auto fp8, auto f16) {
         auto run = [&](auto d) {
             constexpr int D = decltype(d)::value;
-            kv_split_kernel<D, fp8.value, f16.value><<<(uint32_t)wgs, 256, 0, s>>>(c, a, 2);
-            kv_join_kernel<D, f16.value><<<(uint32_t)(c.B * c.H), 256, 0, s>>>(c, a);
+            kv_split_kernel<D, fp8.value, f16.value><<<(uint32_t)wgs, 256, 0, s>>>(c, a, cut);
             if (tiles) {
                 AttnArgs t = a;
                 WsCarve w{(char*)workspace, (size_t)workspace_bytes, head};

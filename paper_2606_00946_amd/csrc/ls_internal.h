@@ -387,6 +387,7 @@ hipError_t launch_kv_append(const KvView& c, const KvRope& r, const void* k, int
                             int64_t v_stride, const void* q, int64_t q_stride, int32_t Hq, void* q_out,
                             int64_t q_out_stride, int n_cu, hipStream_t s);
 hipError_t launch_kv_read(const KvView& c, void* k_out, void* v_out, hipStream_t s);
+hipError_t launch_kv_workspace_init(void* workspace, hipStream_t s);
 hipError_t launch_kv_attention(const KvView& c, const void* q, int64_t q_stride, int32_t Hq, float scale,
                                int32_t window, int32_t sinks, void* out, int64_t out_stride, void* workspace,
                                int64_t workspace_bytes, int n_cu, hipStream_t s);

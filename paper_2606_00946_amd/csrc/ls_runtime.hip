@@ -86,6 +86,7 @@ struct ls_ctx {
     // partial sums of ls_kv_attention's split rows
     void* kv_ws = nullptr;
     size_t kv_ws_cap = 0;
+    bool kv_ws_ready = false;   // its counts are cleared
     // online-learning data path (device pools, host-side counters)
     struct Buffer {
         int32_t fifo_cap = 0, rep_cap = 0, fifo_count = 0, fifo_head = 0, rep_count = 0;
@@ -1484,7 +1485,11 @@ int ls_kv_attention(ls_ctx* c, const ls_kv_cache* cache, const ls_kv_batch* batc
     DeviceScope dev(c->device);
     if (!dev.ok) return fail(c, LS_ERR_DEVICE, "cannot select device %d", c->device);
     hipStream_t s = (hipStream_t)stream;
-    if ((rc = grow(c, &c->kv_ws, &c->kv_ws_cap, LS_KV_WORKSPACE_BYTES, s))) return rc;
+    if (!c->kv_ws_ready) {
+        if ((rc = grow(c, &c->kv_ws, &c->kv_ws_cap, LS_KV_WORKSPACE_BYTES, s))) return rc;
+        LS_HIP(c, ls::launch_kv_workspace_init(c->kv_ws, s));
+        c->kv_ws_ready = true;
+    }
     Timed t(c, K_KV_ATTENTION, s);
     const hipError_t e = ls::launch_kv_attention(w, q, q_stride, n_q_heads, scale, window, sinks, out, out_stride,
                                                  c->kv_ws, (int64_t)c->kv_ws_cap, c->n_cu, s);
