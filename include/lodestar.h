@@ -524,11 +524,12 @@ int ls_swap_model(ls_ctx* ctx, void* serve_stream, void* train_stream);
  *   k_scale, v_scale  fp32 [n_pages x n_kv_heads]: one scale for each page and head;
  *                a code c stands for c * scale.
  * ls_kv_batch  the sequences of a call and their new tokens (host struct of device arrays):
- *   n_seqs, n_tokens, pages_stride, max_new   host values; max_new bounds any sequence's new tokens
+ *   n_seqs, n_tokens, pages_stride, max_new   host values, n_tokens and pages_stride * page_tokens up to 2^30;
+ *                max_new bounds any sequence's new tokens
  *   dtype        of the 16-bit tensors of the call: LS_BF16 or LS_FP16
  *   new_off      int32 [n_seqs + 1], 0 = new_off[0] <= ... <= new_off[n_seqs] = n_tokens: sequence b's
  *                new tokens are rows new_off[b] .. new_off[b+1] of the call's tensors (none: left out)
- *   past         int32 [n_seqs] >= 0: tokens of the sequence before them; new row j is at position past[b] + j
+ *   past         int32 [n_seqs] in [0, 2^30]: tokens of the sequence before them; new row j is at position past[b] + j
  *   pages        int32 [n_seqs x pages_stride]: token t of sequence b is on page pages[b][t / page_tokens].
  *                An id outside [0, n_pages) is an absent page (e.g. -1, given back): its tokens are
  *                neither written nor visible.  The same holds past the end of the table.

@@ -40,17 +40,20 @@ struct Span {
     __device__ __forceinline__ int32_t tile(int32_t i) const { return i < n_sink ? i : win + (i - n_sink); }
 };
 
-__device__ __forceinline__ Span span_of(const KvView& c, const AttnArgs& a, int64_t past, int32_t rows) {
-    const int64_t end = min(past + rows, (int64_t)c.W << c.page_shift);
-    int64_t lo = 0;
-    if (a.window > 0) lo = min(max(past + 1 - a.window, (int64_t)0), end);
+__device__ __forceinline__ Span span_of(const KvView& c, const AttnArgs& a, int32_t past, int32_t rows) {
+    const int32_t end = min(past + rows, c.limit);
+    const int32_t lo = a.window > 0 ? min(max(past + 1 - a.window, 0), end) : 0;
     Span s;
-    s.win = (int32_t)(lo >> 4);
-    s.n_sink = (int32_t)((min((int64_t)a.sinks, lo) + 15) >> 4);
+    s.win = lo >> 4;
+    s.n_sink = (min(a.sinks, lo) + 15) >> 4;
     if (s.n_sink >= s.win) s.n_sink = s.win = 0;
-    s.n = s.n_sink + (int32_t)((end + 15) >> 4) - s.win;
+    s.n = s.n_sink + ((end + 15) >> 4) - s.win;
     return s;
 }
+
+// Positions fit 32 bits: tables end at 2^30 tokens, and a past beyond that counts as that.
+constexpr int32_t kMaxPast = 1 << 30;
+__device__ __forceinline__ int32_t past_of(const KvView& c, int b) { return min(max(c.past[b], 0), kMaxPast); }
 
 // Which of a block's 16 tokens a row sees: up to `last`, and those after `gone` or
 // before `sink`.  Bounds are relative to the block, so 32 bits do; the tests are
@@ -59,14 +62,41 @@ struct Sight {
     int32_t last, gone, sink;
     __device__ __forceinline__ bool sees(int i) const { return (i <= last) & ((i > gone) | (i < sink)); }
 };
-__device__ __forceinline__ Sight sight(const AttnArgs& a, int32_t page, int64_t pos, int64_t tok) {
-    auto near = [](int64_t x) { return (int32_t)min(max(x, (int64_t)-1), (int64_t)16); };
+__device__ __forceinline__ Sight sight(const AttnArgs& a, int32_t page, int32_t pos, int32_t tok) {
     Sight s;
-    s.last = page < 0 ? -1 : near(pos - tok);
-    s.gone = a.window > 0 ? near(pos - a.window - tok) : -1;
-    s.sink = near(a.sinks - tok);
+    s.last = page < 0 ? -1 : pos - tok;
+    s.gone = a.window > 0 ? pos - a.window - tok : -1;
+    s.sink = a.sinks - tok;
     return s;
 }
+
+// The pages of one sequence and kv head: where a 16-token block of it lies.
+struct Blocks {
+    const int32_t* pages;            // the sequence's row of the table
+    int32_t n_blocks;                // blocks that the row covers
+    int32_t n_pages, shift, mask;    // 16-token blocks of a page: 2^shift
+    int64_t page_bytes;
+    int32_t block_bytes, H;
+    const uint8_t *k, *v;
+    const float *ks, *vs;
+    __device__ __forceinline__ Blocks(const KvView& c, int b, int h)
+        : pages(c.pages + (int64_t)b * c.W), n_blocks(c.limit >> 4), n_pages((int32_t)c.n_pages), shift(c.page_shift - 4),
+          mask((c.page >> 4) - 1), page_bytes((int64_t)c.H * c.page * c.D), block_bytes(16 * c.D), H(c.H),
+          k(c.k + (int64_t)h * c.page * c.D), v(c.v + (int64_t)h * c.page * c.D), ks(c.ks + h), vs(c.vs + h) {}
+    // Page of block `blk`, or -1; always a load, so that no branch comes between the loads around it.
+    __device__ __forceinline__ int32_t page(int32_t blk, bool wanted) const {
+        const int32_t p = uniform_load(pages + (min(blk, n_blocks - 1) >> shift));
+        return (wanted & ((uint32_t)p < (uint32_t)n_pages)) ? p : -1;
+    }
+    // Offset of its codes; of some codes for an absent one.
+    __device__ __forceinline__ int64_t at(int32_t page, int32_t blk) const {
+        return (int64_t)max(page, 0) * page_bytes + (blk & mask) * block_bytes;
+    }
+    __device__ __forceinline__ float scale(const float* s, int32_t page) const {
+        const float x = uniform_load(s + (int64_t)max(page, 0) * H);
+        return page >= 0 ? x : 1.0f;
+    }
+};
 
 constexpr int kFewRows = 16;         // rows of a kv head that kv_split_kernel takes
 constexpr int kMaxParts = 8192;        // of a launch of kv_split_kernel that cuts segments
@@ -74,7 +104,7 @@ constexpr int kUnit = 8;             // 16-token blocks of a work unit: two for 
 constexpr int kJoin = 16;            // parts that one workgroup adds
 // Workgroups of kv_split_kernel on a compute unit, by its registers.
 template <int D>
-constexpr int kSplitPerCu = D == 64 ? 4 : D == 128 ? 3 : 1;
+constexpr int kSplitPerCu = D == 64 ? 4 : D == 128 ? 2 : 1;
 constexpr int kMinUnits = 8;        // no segment is cut finer
 constexpr float kNoMax = -1e30f;     // running maximum of nothing
 constexpr float kTop = 7.0f;         // weights start below 2^7 ...
@@ -87,7 +117,7 @@ struct Seq {
 __device__ __forceinline__ Seq seq_of(const KvView& c, const AttnArgs& a, int b) {
     Seq s;
     seq_rows(c, b, s.t0, s.n);
-    s.past = max(c.past[b], 0);
+    s.past = past_of(c, b);
     s.units = 0;
     if (s.n != 0 && (int64_t)s.n * a.G <= a.few)
         s.units = max((span_of(c, a, s.past, s.n).n + kUnit - 1) / kUnit, 1);
@@ -308,138 +338,143 @@ __global__ __launch_bounds__(256, kSplitPerCu<D>) void kv_split_kernel(KvView c,
             if (seq.units == 0) continue;
         }
         const int t0 = seq.t0, n = seq.n;
-        const int64_t past = seq.past;
+        const int32_t past = seq.past;
         const Span span = span_of(c, a, past, n);
-        const int64_t end_tok = min(past + n, (int64_t)c.W << c.page_shift);
-        const int32_t u0 = (int32_t)((int64_t)seq.units * piece / pieces);
-        const int32_t u1 = (int32_t)((int64_t)seq.units * (piece + 1) / pieces);
+        const int32_t end_tok = min(past + n, c.limit);
+        // the first `seq.units % pieces` parts are a unit longer
+        const int32_t len = (int32_t)((uint32_t)seq.units / (uint32_t)pieces), more = seq.units - len * pieces;
+        const int32_t u0 = piece * len + min(piece, more), u1 = u0 + len + (piece < more ? 1 : 0);
         const int rows = n * a.G;
-        const int64_t pos = past + col / a.G;                // the column's position
-        const int64_t pos_last = past + n - 1;
+        const int32_t pos = past + col / a.G;                // the column's position
+        const int32_t pos_last = past + n - 1;
 
         half8 q[ND][2];
         const float undo = load_queries<D, F16>(a, h, t0, col, rows, q);
         const float s2 = a.scale2 * undo;
 
-        // pages of step i's two blocks, and what is known of them
+        // step i's two blocks
+        const Blocks blocks(c, b, h);
+        const int steps = u1 - u0;
         struct Meta { int32_t page[2]; float ks[2], vs[2]; };
         auto tile_of = [&](int i, int e) { return (u0 + i) * kUnit + wave * 2 + e; };
         auto find_page = [&](int i, Meta& m) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int t = tile_of(i, e);
-                int32_t p = -1;
-                if (i < u1 - u0 && t < span.n) {
-                    const int32_t j = span.tile(t) >> (c.page_shift - 4);
-                    p = uniform_load(c.pages + (int64_t)b * c.W + j);
-                    if (p >= c.n_pages) p = -1;
-                }
-                m.page[e] = p;
-            }
+            for (int e = 0; e < 2; ++e) m.page[e] = blocks.page(span.tile(tile_of(i, e)), (i < steps) & (tile_of(i, e) < span.n));
         };
         auto find_scales = [&](Meta& m) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                m.ks[e] = m.vs[e] = 1.0f;
-                if (m.page[e] >= 0) {
-                    m.ks[e] = uniform_load(c.ks + (int64_t)m.page[e] * c.H + h);
-                    m.vs[e] = uniform_load(c.vs + (int64_t)m.page[e] * c.H + h);
-                }
+                m.ks[e] = blocks.scale(blocks.ks, m.page[e]);
+                m.vs[e] = blocks.scale(blocks.vs, m.page[e]);
             }
         };
         struct Raw { uint4v k[2][ND], v[2][ND]; };
-        auto fetch = [&](int i, const Meta& m, Raw& r) {
+        // (of page 0 for an absent block: hidden from the sums)
+        auto fetch = [&](int i, const Meta& m, const uint8_t* codes, uint32_t lane_at, uint4v (&r)[2][ND]) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int t = tile_of(i, e);
-                const int64_t base = m.page[e] < 0 ? 0 : block_at(c, m.page[e], h, span.tile(t) & ((c.page >> 4) - 1));
-                const uint8_t* kp = c.k + base + col * 64 + g * 16;
-                const uint8_t* vp = c.v + base + lane * 16;
+                const uint8_t* p = codes + blocks.at(m.page[e], span.tile(tile_of(i, e))) + lane_at;
 #pragma unroll
-                for (int dt = 0; dt < ND; ++dt) {
-                    r.k[e][dt] = *reinterpret_cast<const uint4v*>(kp + dt * 1024);
-                    r.v[e][dt] = *reinterpret_cast<const uint4v*>(vp + dt * 1024);
-                }
+                for (int dt = 0; dt < ND; ++dt) r[e][dt] = *reinterpret_cast<const uint4v*>(p + dt * 1024);
             }
         };
+        auto fetch_k = [&](int i, const Meta& m, Raw& r) { fetch(i, m, blocks.k, col * 64 + g * 16, r.k); };
+        auto fetch_v = [&](int i, const Meta& m, Raw& r) { fetch(i, m, blocks.v, lane * 16, r.v); };
         float m_run = kNoMax, l_run = 0.0f;
         float4v o[ND][4] = {};
-        auto compute = [&](int i, const Meta& m, Raw& r) {
-            if (m.page[0] < 0 && m.page[1] < 0) return;
-            float x[2][4], mx = -INFINITY;
-            float iv[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float4v s = {0, 0, 0, 0};
+        // One step.
+        auto step = [&](int i, const Meta& m, Raw& r) {
+            float4v s[2] = {};
+            {
 #pragma unroll
                 for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
                     for (int k = 0; k < 2; ++k)
-                        s = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-                            code_halves8<FP8>(r.k[e][dt][2 * k], r.k[e][dt][2 * k + 1]), q[dt][k], s, 0, 0, 0);
-                const float f = m.ks[e] * s2, lv = __builtin_amdgcn_logf(m.vs[e]);
-                iv[e] = __builtin_amdgcn_rcpf(m.vs[e]);
-                const int64_t tok = (int64_t)span.tile(tile_of(i, e)) * 16;
-                const bool all = m.page[e] >= 0 && tok + 15 <= past &&
-                                 (a.window == 0 || tok > pos_last - a.window || tok + 15 < a.sinks);
-                if (all) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) x[e][k] = fmaf(s[k], f, lv);
-                } else {
-                    const Sight see = sight(a, m.page[e], pos, tok);
+                        for (int e = 0; e < 2; ++e)
+                            s[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                                code_halves8<FP8>(r.k[e][dt][2 * k], r.k[e][dt][2 * k + 1]), q[dt][k], s[e], 0, 0, 0);
+            }
+            {
+                float x[2][4], f[2], lv[2], iv[2];
+                int32_t tok[2];
+                bool all = true;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) x[e][k] = see.sees(4 * g + k) ? fmaf(s[k], f, lv) : -INFINITY;
-                    // codes of nobody's tokens may be NaN: out of the product
-                    const int64_t left = m.page[e] >= 0 ? end_tok - (tok + 4 * g) : 0;
-                    const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * (int)left)) - 1;
-#pragma unroll
-                    for (int dt = 0; dt < ND; ++dt) r.v[e][dt] &= keep;
+                for (int e = 0; e < 2; ++e) {
+                    f[e] = m.ks[e] * s2;
+                    lv[e] = __builtin_amdgcn_logf(m.vs[e]);
+                    iv[e] = __builtin_amdgcn_rcpf(m.vs[e]);
+                    tok[e] = span.tile(tile_of(i, e)) * 16;
+                    all &= (m.page[e] >= 0) & (tok[e] + 15 <= past) &
+                           ((a.window == 0) | (tok[e] > pos_last - a.window) | (tok[e] + 15 < a.sinks));
                 }
 #pragma unroll
-                for (int k = 0; k < 4; ++k) mx = fmaxf(mx, x[e][k]);
-            }
-            if (__any(mx > m_run + kGrow)) {
-                mx = fmaxf(mx, __shfl_xor(mx, 16));
-                mx = fmaxf(mx, __shfl_xor(mx, 32));
-                const float m2 = fmaxf(m_run, mx);
-                const float f = __builtin_amdgcn_exp2f(m_run - m2);
-                m_run = m2;
-                l_run *= f;
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) x[e][k] = fmaf(s[e][k], f[e], lv[e]);
+                if (!all) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const Sight see = sight(a, m.page[e], pos, tok[e]);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) x[e][k] = see.sees(4 * g + k) ? x[e][k] : -INFINITY;
+                        // codes of nobody's tokens may be NaN: out of the product
+                        const int32_t left = m.page[e] >= 0 ? end_tok - (tok[e] + 4 * g) : 0;
+                        const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
+#pragma unroll
+                        for (int dt = 0; dt < ND; ++dt) r.v[e][dt] &= keep;
+                    }
+                }
+                float mx = -INFINITY;
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mx = fmaxf(mx, x[e][k]);
+                if (__any(mx > m_run + kGrow)) {
+                    mx = fmaxf(mx, __shfl_xor(mx, 16));
+                    mx = fmaxf(mx, __shfl_xor(mx, 32));
+                    const float top = fmaxf(m_run, mx);
+                    const float f = __builtin_amdgcn_exp2f(m_run - top);
+                    m_run = top;
+                    l_run *= f;
+#pragma unroll
+                    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) o[dt][k] *= f;
+                }
+                half8 p;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float w[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) w[k] = __builtin_amdgcn_exp2f(x[e][k] - (m_run - kTop));
+                    l_run = fmaf((w[0] + w[1]) + (w[2] + w[3]), iv[e], l_run);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) p[4 * e + k] = (_Float16)w[k];
+                }
 #pragma unroll
                 for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) o[dt][k] *= f;
+                    for (int k = 0; k < 4; ++k)
+                        o[dt][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                            code_halves8<FP8>(r.v[0][dt][k], r.v[1][dt][k]), p, o[dt][k], 0, 0, 0);
             }
-            half8 p;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float w[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) w[k] = __builtin_amdgcn_exp2f(x[e][k] - (m_run - kTop));
-                l_run = fmaf((w[0] + w[1]) + (w[2] + w[3]), iv[e], l_run);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) p[4 * e + k] = (_Float16)w[k];
-            }
-#pragma unroll
-            for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    o[dt][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-                        code_halves8<FP8>(r.v[0][dt][k], r.v[1][dt][k]), p, o[dt][k], 0, 0, 0);
         };
 
-        const int steps = u1 - u0;
+        // pages are looked up two steps ahead, codes and scales fetched one
         Meta m0, m1, m2;
         Raw r0, r1;
         find_page(0, m0);
         find_page(1, m1);
         find_scales(m0);
-        fetch(0, m0, r0);
+        fetch_k(0, m0, r0);
+        fetch_v(0, m0, r0);
         for (int i = 0; i < steps; ++i) {
             find_page(i + 2, m2);
             find_scales(m1);
-            fetch(i + 1, m1, r1);
-            compute(i, m0, r0);
+            fetch_k(i + 1, m1, r1);
+            fetch_v(i + 1, m1, r1);
+            step(i, m0, r0);
             m0 = m1;
             m1 = m2;
             r0 = r1;
@@ -524,7 +559,7 @@ struct TileWork {
     Span span;
     int32_t u0, u1, shares;
 };
-__device__ __forceinline__ TileWork tile_work(const KvView& c, const AttnArgs& a, int64_t past, int r0, int rows,
+__device__ __forceinline__ TileWork tile_work(const KvView& c, const AttnArgs& a, int32_t past, int r0, int rows,
                                               int sp, int splits) {
     const int tok0 = r0 / a.G, tok1 = (r0 + rows - 1) / a.G;
     TileWork w;
@@ -562,19 +597,19 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tile_kernel(KvView c
     int b, t0, r0;
     const int rows = tile_of_slot(c, a, slot, b, t0, r0);
     if (rows == 0) return;
-    const int64_t past = max(c.past[b], 0);
+    const int32_t past = past_of(c, b);
     const TileWork work = tile_work(c, a, past, r0, rows, sp, splits);
     const Span span = work.span;
     if (sp >= work.shares) return;
     int n_all, t_;
     seq_rows(c, b, t_, n_all);
-    const int64_t end_tok = min(past + n_all, (int64_t)c.W << c.page_shift);
+    const int32_t end_tok = min(past + n_all, c.limit);
 
     // this wave's rows and the positions they span
     const int w0 = wave * 32, wrows = min(max(rows - w0, 0), 32);
     const int row = r0 + w0 + col;
-    const int64_t pos = past + row / a.G;
-    const int64_t pos_min = past + (r0 + w0) / a.G, pos_max = past + (r0 + w0 + max(wrows, 1) - 1) / a.G;
+    const int32_t pos = past + row / a.G;
+    const int32_t pos_min = past + (r0 + w0) / a.G, pos_max = past + (r0 + w0 + max(wrows, 1) - 1) / a.G;
 
     half8 q[NK];
     float s2 = fabsf(a.scale2);
@@ -610,50 +645,37 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tile_kernel(KvView c
     }
     s2 = fmaxf(s2, 1e-30f);          // a hidden token's score stays -inf under it
 
+    const Blocks blocks(c, b, h);
     struct Meta { int32_t page[4]; float ks[4], vs[4]; };
     auto find_pages = [&](int t, Meta& m) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int i = t * 4 + e;
-            int32_t p = -1;
-            if (t < work.u1 && i < span.n) {
-                p = uniform_load(c.pages + (int64_t)b * c.W + (span.tile(i) >> (c.page_shift - 4)));
-                if (p >= c.n_pages) p = -1;
-            }
-            m.page[e] = p;
-        }
+        for (int e = 0; e < 4; ++e)
+            m.page[e] = blocks.page(span.tile(t * 4 + e), (t < work.u1) & (t * 4 + e < span.n));
     };
     auto find_scales = [&](Meta& m) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            m.ks[e] = m.vs[e] = 1.0f;
-            if (m.page[e] >= 0) {
-                m.ks[e] = uniform_load(c.ks + (int64_t)m.page[e] * c.H + h);
-                m.vs[e] = uniform_load(c.vs + (int64_t)m.page[e] * c.H + h);
-            }
+            m.ks[e] = blocks.scale(blocks.ks, m.page[e]);
+            m.vs[e] = blocks.scale(blocks.vs, m.page[e]);
         }
     };
     // the wave's share of a step: block `wave` of the four
     uint4v rk[ND], rv[ND];
+    uint32_t keep = 0;
     auto fetch = [&](int t, const Meta& m) {
         const int32_t page = wave == 0 ? m.page[0] : wave == 1 ? m.page[1] : wave == 2 ? m.page[2] : m.page[3];
         const int32_t blk = span.tile(t * 4 + wave);
-        const int64_t base = page < 0 ? 0 : block_at(c, page, h, blk & ((c.page >> 4) - 1));
-        const uint8_t* kp = c.k + base + (lane & 15) * 64 + (lane >> 4) * 16;
-        const uint8_t* vp = c.v + base + lane * 16;
+        const int64_t base = blocks.at(page, blk);
+        const uint8_t* kp = blocks.k + base + (lane & 15) * 64 + (lane >> 4) * 16;
+        const uint8_t* vp = blocks.v + base + lane * 16;
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) {
             rk[dt] = *reinterpret_cast<const uint4v*>(kp + dt * 1024);
             rv[dt] = *reinterpret_cast<const uint4v*>(vp + dt * 1024);
         }
         // codes of nobody's tokens may be NaN: out of the product
-        const int64_t tok = (int64_t)blk * 16 + (lane >> 4) * 4;
-        if (page < 0 || (int64_t)blk * 16 + 16 > end_tok) {
-            const int64_t left = page >= 0 ? end_tok - tok : 0;
-            const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * (int)left)) - 1;
-#pragma unroll
-            for (int dt = 0; dt < ND; ++dt) rv[dt] &= keep;
-        }
+        const int32_t left = page >= 0 ? end_tok - (blk * 16 + (lane >> 4) * 4) : 0;
+        keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
     };
     auto stage = [&](int buf) {
         // keys: lane (token lane % 16, dimensions 16 (lane / 16) ..) holds both halves of a product step's operand
@@ -668,6 +690,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tile_kernel(KvView c
         // groups of two dimensions, one operand register set each
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) {
+            rv[dt] &= keep;
             const auto x = __builtin_amdgcn_permlane32_swap(rv[dt][0], rv[dt][2], false, false);
             const auto y = __builtin_amdgcn_permlane32_swap(rv[dt][1], rv[dt][3], false, false);
             uint4v* d = &lv[buf][wave][dt * 2 + hi][((lane >> 4) & 1) * 32 + (lane & 15)];
@@ -680,14 +703,14 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tile_kernel(KvView c
     float16v o[NV] = {};
     auto compute = [&](int t, int buf, const Meta& m) {
         bool any = false, full[4];
-        int64_t tok[4];
+        int32_t tok[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            tok[e] = (int64_t)span.tile(t * 4 + e) * 16;
-            any |= m.page[e] >= 0 && tok[e] <= pos_max &&
-                   (a.window == 0 || tok[e] + 15 > pos_min - a.window || tok[e] < a.sinks);
-            full[e] = m.page[e] >= 0 && tok[e] + 15 <= pos_min &&
-                      (a.window == 0 || tok[e] > pos_max - a.window || tok[e] + 15 < a.sinks);
+            tok[e] = span.tile(t * 4 + e) * 16;
+            any |= (m.page[e] >= 0) & (tok[e] <= pos_max) &
+                   ((a.window == 0) | (tok[e] + 15 > pos_min - a.window) | (tok[e] < a.sinks));
+            full[e] = (m.page[e] >= 0) & (tok[e] + 15 <= pos_min) &
+                      ((a.window == 0) | (tok[e] > pos_max - a.window) | (tok[e] + 15 < a.sinks));
         }
         if (wrows == 0 || !any) return;
         float16v s[2] = {};
@@ -813,7 +836,7 @@ __global__ __launch_bounds__(256) void kv_tile_join_kernel(KvView c, AttnArgs a,
     const int rows = tile_of_slot(c, a, slot, b, t0, r0);
     const int i = piece * 8 + (threadIdx.x >> 5), d0 = (threadIdx.x & 31) * (D / 32);
     if (i >= rows) return;
-    const int shares = tile_work(c, a, max(c.past[b], 0), r0, rows, 0, splits).shares;
+    const int shares = tile_work(c, a, past_of(c, b), r0, rows, 0, splits).shares;
     if (shares == 1) return;
     float m = kNoMax, l = 0.0f, v[D / 32] = {};
     for (int sp = 0; sp < shares; ++sp) {
@@ -868,12 +891,12 @@ hipError_t launch_kv_attention(const KvView& c, const void* q, int64_t q_stride,
     WsCarve ws{(char*)workspace, (size_t)workspace_bytes};
     a.arrived = ws.take<uint32_t>(kMaxParts * 2);
     const size_t head = ws.off;
-    // as many parts as workgroups fit the device, and twice the segments where these are more; segments stay whole
+    // as many parts as workgroups fit the device, and 2.5 for each segment where that is more; segments stay whole
     // where the workspace does not hold that many parts
     const int64_t segments = (int64_t)c.B * c.H, fit = (int64_t)n_cu * (c.D == 64 ? kSplitPerCu<64> : c.D == 128 ? kSplitPerCu<128> : kSplitPerCu<256>);
     const int64_t room = std::min<int64_t>((workspace_bytes - (int64_t)head - 4096) / (kFewRows * (c.D + 2) * 4), kMaxParts);
     const bool cut = segments * 3 <= room * 2;
-    const int64_t wgs = cut ? std::min(std::max(fit, segments * 2), room) : segments;
+    const int64_t wgs = cut ? std::min(std::max(fit, segments * 5 / 2), room) : segments;
     if (wgs >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
     if (cut) {
         a.part_ml = ws.take<float2v>(wgs * kFewRows);

@@ -377,6 +377,7 @@ struct KvView {
     const int32_t *off, *past, *pages;
     int32_t B, T, W;                // sequences, rows, pages of a table row
     int32_t max_new;                // no sequence has more rows
+    int32_t limit;                  // tokens that a table row covers, at most 2^30
     bool fp8, f16;                  // code type; 16-bit type of the call's tensors
 };
 struct KvRope {

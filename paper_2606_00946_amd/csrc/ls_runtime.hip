@@ -1383,6 +1383,9 @@ int kv_view(ls_ctx* c, const ls_kv_cache* kv, const ls_kv_batch* b, ls::KvView* 
             return fail(c, LS_ERR_INVALID, "new_off, past and pages must be non-NULL");
         if (b->pages_stride < 1) return fail(c, LS_ERR_INVALID, "pages_stride must be >= 1");
         if (b->max_new < 1) return fail(c, LS_ERR_INVALID, "max_new must be >= 1");
+        if (b->n_tokens >= 1 << 30) return fail(c, LS_ERR_INVALID, "n_tokens must be below 2^30");
+        if ((int64_t)b->pages_stride * kv->page_tokens > 1 << 30)
+            return fail(c, LS_ERR_INVALID, "pages_stride * page_tokens must be at most 2^30");
     }
     ls::KvView v;
     v.k = (uint8_t*)kv->k;
@@ -1401,6 +1404,7 @@ int kv_view(ls_ctx* c, const ls_kv_cache* kv, const ls_kv_batch* b, ls::KvView* 
     v.T = b->n_tokens;
     v.W = b->pages_stride;
     v.max_new = std::min(b->max_new, b->n_tokens);
+    v.limit = (int32_t)((int64_t)b->pages_stride * kv->page_tokens);
     v.fp8 = kv->dtype == LS_KV_FP8;
     v.f16 = b->dtype == LS_FP16;
     *out = v;
