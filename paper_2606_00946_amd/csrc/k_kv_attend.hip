@@ -108,6 +108,7 @@ constexpr int kSplitPerCu = D == 64 ? 4 : D == 128 ? 2 : 1;
 constexpr int kMinUnits = 8;        // no segment is cut finer
 constexpr float kNoMax = -1e30f;     // running maximum of nothing
 constexpr float kTop = 7.0f;         // weights start below 2^7 ...
+constexpr float kMostWeight = 0x1p+15f; // of the sum of a lane's weights, before the maximum moves
 constexpr float kGrow = 8.0f;        // ... and the maximum moves when one would pass 2^15
 
 // A sequence of the call as kv_split_kernel sees it; units of one kv head, 0: not that kernel's.
@@ -645,33 +646,43 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tile_kernel(KvView c
     }
     s2 = fmaxf(s2, 1e-30f);          // a hidden token's score stays -inf under it
 
+    // Blocks (of the span) that all of the wave's rows see whole, but for the sinks, and that any row sees.
+    const int32_t base_i = span.n_sink - span.win;
+    const int32_t full_lo = a.window > 0 ? max(span.n_sink, ((pos_max - a.window + 16) >> 4) + base_i) : 0;
+    const int32_t full_hi = ((pos_min - 15) >> 4) + base_i;
+    const int32_t any_lo = a.window > 0 ? max(span.n_sink, ((pos_min - a.window + 1) >> 4) + base_i) : 0;
+    const int32_t any_hi = (pos_max >> 4) + base_i;
+    const int32_t sink_hi = a.window > 0 ? (min(a.sinks, c.limit) + 15) >> 4 : 0;
+
+    // A step's four pages and eight scales are one register each: lane e holds block e's page, and its key scale, lane
+    // 4 + e its value scale.
     const Blocks blocks(c, b, h);
-    struct Meta { int32_t page[4]; float ks[4], vs[4]; };
-    auto find_pages = [&](int t, Meta& m) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            m.page[e] = blocks.page(span.tile(t * 4 + e), (t < work.u1) & (t * 4 + e < span.n));
+    const int e4 = lane & 3;
+    auto load_page = [&](int t) {
+        return blocks.pages[min(span.tile(t * 4 + e4), blocks.n_blocks - 1) >> blocks.shift];
     };
-    auto find_scales = [&](Meta& m) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            m.ks[e] = blocks.scale(blocks.ks, m.page[e]);
-            m.vs[e] = blocks.scale(blocks.vs, m.page[e]);
-        }
+    auto checked = [&](int32_t page, int t) {
+        const bool there = (t < work.u1) & (t * 4 + e4 < span.n) & ((uint32_t)page < (uint32_t)blocks.n_pages);
+        return there ? page : -1;
     };
+    const float* scales = lane & 4 ? blocks.vs : blocks.ks;
+    auto load_scale = [&](int32_t page) { return scales[(int64_t)max(page, 0) * blocks.H]; };
+    auto of_lane = [](float x, int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l)); };
+
     // the wave's share of a step: block `wave` of the four
     uint4v rk[ND], rv[ND];
     uint32_t keep = 0;
-    auto fetch = [&](int t, const Meta& m) {
-        const int32_t page = wave == 0 ? m.page[0] : wave == 1 ? m.page[1] : wave == 2 ? m.page[2] : m.page[3];
+    auto fetch = [&](int t, int32_t pages) {
+        const int32_t page = __builtin_amdgcn_readlane(pages, wave);
         const int32_t blk = span.tile(t * 4 + wave);
         const int64_t base = blocks.at(page, blk);
-        const uint8_t* kp = blocks.k + base + (lane & 15) * 64 + (lane >> 4) * 16;
-        const uint8_t* vp = blocks.v + base + lane * 16;
+        const uint8_t* kp = blocks.k + base;
+        const uint8_t* vp = blocks.v + base;
+        const uint32_t k_at = (lane & 15) * 64 + (lane >> 4) * 16, v_at = lane * 16;
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) {
-            rk[dt] = *reinterpret_cast<const uint4v*>(kp + dt * 1024);
-            rv[dt] = *reinterpret_cast<const uint4v*>(vp + dt * 1024);
+            rk[dt] = *reinterpret_cast<const uint4v*>(kp + k_at + dt * 1024);
+            rv[dt] = *reinterpret_cast<const uint4v*>(vp + v_at + dt * 1024);
         }
         // codes of nobody's tokens may be NaN: out of the product
         const int32_t left = page >= 0 ? end_tok - (blk * 16 + (lane >> 4) * 4) : 0;
@@ -701,44 +712,78 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tile_kernel(KvView c
 
     float m_run = kNoMax, l_run = 0.0f;
     float16v o[NV] = {};
-    auto compute = [&](int t, int buf, const Meta& m) {
-        bool any = false, full[4];
-        int32_t tok[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            tok[e] = span.tile(t * 4 + e) * 16;
-            any |= (m.page[e] >= 0) & (tok[e] <= pos_max) &
-                   ((a.window == 0) | (tok[e] + 15 > pos_min - a.window) | (tok[e] < a.sinks));
-            full[e] = (m.page[e] >= 0) & (tok[e] + 15 <= pos_min) &
-                      ((a.window == 0) | (tok[e] > pos_max - a.window) | (tok[e] + 15 < a.sinks));
-        }
-        if (wrows == 0 || !any) return;
+    // One step: scores, weights, product.  LDS reads are issued well before their products (the scheduling barriers keep
+    // them there).
+    auto compute = [&](int t, int buf, int32_t pages, float scale) {
+        const uint32_t have = (uint32_t)__ballot(pages >= 0) & 15u;
+        const int i0 = t * 4, i3 = i0 + 3;
+        if ((wrows == 0) | (have == 0) | (i0 > any_hi) | ((i3 < any_lo) & (i0 >= sink_hi))) return;
+        scale = pages >= 0 ? scale : 1.0f;
+        const float log_scale = __builtin_amdgcn_logf(scale), inv_scale = __builtin_amdgcn_rcpf(scale);
         float16v s[2] = {};
+        constexpr int KC = D == 256 ? 4 : NK, VC = D == 256 ? 1 : 2;     // products, and blocks, whose operands are read at once
 #pragma unroll
-        for (int k = 0; k < NK; ++k)
+        for (int k0 = 0; k0 < NK; k0 += KC) {
+            uint4v kf[KC][2];
 #pragma unroll
-            for (int g = 0; g < 2; ++g)
-                s[g] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, lk[buf][g][k][lane]), q[k], s[g],
-                                                              0, 0, 0);
-        float f[4], lg[4], mx = -INFINITY;
+            for (int k = 0; k < KC; ++k)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (!full[e]) {
-                const Sight v = sight(a, m.page[e], pos, tok[e]);
+                for (int g = 0; g < 2; ++g) kf[k][g] = lk[buf][g][k0 + k][lane];
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int k = 0; k < KC; ++k)
+#pragma unroll
+                for (int g = 0; g < 2; ++g)
+                    s[g] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, kf[k][g]), q[k0 + k], s[g], 0, 0, 0);
+        }
+        uint4v vf[2][VC][NV];                // values of VC blocks, twice
+        auto read_values = [&](int e0) {
+#pragma unroll
+            for (int e = 0; e < VC; ++e)
+#pragma unroll
+                for (int i = 0; i < NV; ++i) vf[(e0 / VC) & 1][e][i] = lv[buf][e0 + e][i][lane];
+        };
+        read_values(0);
+        __builtin_amdgcn_sched_barrier(0);
+        if ((have != 15u) | (i0 < full_lo) | (i3 > full_hi)) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const Sight v = sight(a, have >> e & 1 ? 0 : -1, pos, span.tile(i0 + e) * 16);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float x = s[e >> 1][(e & 1) * 8 + i];
                     s[e >> 1][(e & 1) * 8 + i] = v.sees(8 * (i >> 2) + 4 * hi + (i & 3)) ? x : -INFINITY;
                 }
             }
-            f[e] = m.ks[e] * s2;
-            lg[e] = __builtin_amdgcn_logf(m.vs[e]);
-            float top = s[e >> 1][(e & 1) * 8];
-#pragma unroll
-            for (int i = 1; i < 8; ++i) top = fmaxf(top, s[e >> 1][(e & 1) * 8 + i]);
-            mx = fmaxf(mx, fmaf(top, f[e], lg[e]));
         }
-        if (__any(mx > m_run + kGrow)) {
+        float f[4], sum[4];
+        half8 p[4];
+        auto weigh = [&] {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float off = of_lane(log_scale, 4 + e) - (m_run - kTop);
+                sum[e] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float w = __builtin_amdgcn_exp2f(fmaf(s[e >> 1][(e & 1) * 8 + i], f[e], off));
+                    sum[e] += w;
+                    p[e][i] = (_Float16)w;
+                }
+            }
+        };
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = of_lane(scale, e) * s2;
+        weigh();
+        // weights under the maximum so far; where their sum shows that one may not fit a half, the maximum moves first
+        if (__any((sum[0] + sum[1]) + (sum[2] + sum[3]) > kMostWeight)) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float top = s[e >> 1][(e & 1) * 8];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) top = fmaxf(top, s[e >> 1][(e & 1) * 8 + i]);
+                mx = fmaxf(mx, fmaf(top, f[e], of_lane(log_scale, 4 + e)));
+            }
             mx = fmaxf(mx, __shfl_xor(mx, 32));
             const float m2 = fmaxf(m_run, mx);
             const float r = __builtin_amdgcn_exp2f(m_run - m2);
@@ -746,49 +791,44 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tile_kernel(KvView c
             l_run *= r;
 #pragma unroll
             for (int i = 0; i < NV; ++i) o[i] *= r;
-        }
-        half8 p[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float off = lg[e] - (m_run - kTop);
-            float sum = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float w = __builtin_amdgcn_exp2f(fmaf(s[e >> 1][(e & 1) * 8 + i], f[e], off));
-                sum += w;
-                p[e][i] = (_Float16)w;
-            }
-            l_run = fmaf(sum, __builtin_amdgcn_rcpf(m.vs[e]), l_run);
+            weigh();
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+        for (int e = 0; e < 4; ++e) l_run = fmaf(sum[e], of_lane(inv_scale, 4 + e), l_run);
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, lv[buf][e][i][lane]), p[e], o[i],
-                                                              0, 0, 0);
+        for (int e0 = 0; e0 < 4; e0 += VC) {
+            if (e0 + VC < 4) read_values(e0 + VC);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int e = 0; e < VC; ++e)
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, vf[(e0 / VC) & 1][e][i]),
+                                                                  p[e0 + e], o[i], 0, 0, 0);
+        }
     };
 
-    // pages are looked up three steps ahead, codes fetched two and scales one
-    Meta m0, m1, m2, m3;
-    find_pages(work.u0, m0);
-    find_pages(work.u0 + 1, m1);
-    find_pages(work.u0 + 2, m2);
-    find_scales(m0);
-    fetch(work.u0, m0);
+    // pages are looked up three steps ahead, codes and scales fetched two and codes staged one
+    int32_t page0 = checked(load_page(work.u0), work.u0), page1 = checked(load_page(work.u0 + 1), work.u0 + 1);
+    int32_t next = load_page(work.u0 + 2);
+    float scale0 = load_scale(page0), scale1 = load_scale(page1);
+    fetch(work.u0, page0);
     stage(work.u0 & 1);
-    fetch(work.u0 + 1, m1);
+    fetch(work.u0 + 1, page1);
     __syncthreads();
     for (int t = work.u0; t < work.u1; ++t) {
         // the other buffer's readers passed the barrier that ended the step before
         stage((t + 1) & 1);
-        find_pages(t + 3, m3);
-        find_scales(m1);
-        fetch(t + 2, m2);
-        compute(t, t & 1, m0);
+        const int32_t page2 = checked(next, t + 2);
+        next = load_page(t + 3);
+        const float scale2 = load_scale(page2);
+        fetch(t + 2, page2);
+        compute(t, t & 1, page0, scale0);
         __syncthreads();
-        m0 = m1;
-        m1 = m2;
-        m2 = m3;
+        page0 = page1;
+        page1 = page2;
+        scale0 = scale1;
+        scale1 = scale2;
     }
 
     l_run += __shfl_xor(l_run, 32);
