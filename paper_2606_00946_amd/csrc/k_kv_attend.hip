@@ -31,6 +31,9 @@ struct AttnArgs {
     float* part_o;                   // [parts][16][D]
     float2v* part_ml;                // [parts][16] running maximum and sum
     uint32_t* arrived;               // [parts][2], zero between launches
+    // tiles of many rows whose tokens several workgroups share: [tile][share][kTileRows]
+    float* tile_o;
+    float2v* tile_ml;
 };
 
 // What a sequence's rows see, in 16-token blocks: the first n_sink and those from
@@ -98,8 +101,8 @@ struct Blocks {
     }
 };
 
-constexpr int kFewRows = 16;         // rows of a kv head that kv_split_kernel takes
-constexpr int kMaxParts = 8192;        // of a launch of kv_split_kernel that cuts segments
+constexpr int kFewRows = 16;         // rows of a kv head that split_part takes
+constexpr int kMaxParts = 8192;        // of a launch that cuts segments
 constexpr int kUnit = 8;             // 16-token blocks of a work unit: two for each wave of a workgroup
 constexpr int kJoin = 16;            // parts that one workgroup adds
 // Workgroups of kv_split_kernel on a compute unit, by its registers.
@@ -111,7 +114,7 @@ constexpr float kTop = 7.0f;         // weights start below 2^7 ...
 constexpr float kMostWeight = 0x1p+15f; // of the sum of a lane's weights, before the maximum moves
 constexpr float kGrow = 8.0f;        // ... and the maximum moves when one would pass 2^15
 
-// A sequence of the call as kv_split_kernel sees it; units of one kv head, 0: not that kernel's.
+// A sequence of the call as split_part sees it; units of one kv head, 0: too many rows for it.
 struct Seq {
     int32_t t0, n, past, units;
 };
@@ -271,15 +274,21 @@ __device__ __forceinline__ void add_parts(const AttnArgs& a, uint32_t first, int
 // tokens at a time: scores transposed (tokens x rows), so that their registers are
 // the second operand of the product with the values as they stand; codes go from
 // memory to registers in 16-byte loads, one step ahead of their use.
+template <int D>
+struct SplitLds {
+    float comb[4][16][D + 4];
+    float2v ml[4][16];
+};
 template <int D, bool FP8, bool F16>
-__global__ __launch_bounds__(256, kSplitPerCu<D>) void kv_split_kernel(KvView c, AttnArgs a, bool cut) {
+__device__ __forceinline__ void split_part(const KvView& c, const AttnArgs& a, bool cut, uint32_t block, uint32_t blocks_,
+                                           SplitLds<D>& lds) {
     constexpr int ND = D / 64;
-    __shared__ float comb[4][16][D + 4];
-    __shared__ float2v ml[4][16];
+    auto& comb = lds.comb;
+    auto& ml = lds.ml;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
 
-    // Segments are cut into equal parts of at most `most` units, so that about gridDim.x parts hold all units and a
+    // Segments are cut into equal parts of at most `most` units, so that about as many parts as workgroups hold all units and a
     // long sequence weighs no more on one workgroup than its share (not cut: a part is a segment, found at once).
     uint32_t most = ~0u;
     if (cut) {
@@ -288,12 +297,12 @@ __global__ __launch_bounds__(256, kSplitPerCu<D>) void kv_split_kernel(KvView c,
 #pragma unroll
         for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o);
         const uint64_t all = (uint64_t)uniform((int64_t)total) * c.H;
-        const uint32_t room = gridDim.x - (uint32_t)(c.B * c.H);
+        const uint32_t room = blocks_ - (uint32_t)(c.B * c.H);
         // 2^24 units and more, the largest segment, cut nothing
         const uint64_t each = all >> 31 ? (all + room - 1) / room : ((uint32_t)all + room - 1) / room;
         most = (uint32_t)min(max(each, (uint64_t)kMinUnits), (uint64_t)1 << 24);
     }
-    for (uint32_t part = blockIdx.x;; part += gridDim.x) {
+    for (uint32_t part = block;; part += blocks_) {
         Seq seq;
         int b = 0, h, piece = 0, pieces = 1;
         uint32_t seg = part;             // first part of the segment
@@ -572,7 +581,7 @@ __device__ __forceinline__ TileWork tile_work(const KvView& c, const AttnArgs& a
     return w;
 }
 
-// The tile of slot `slot`: sequence, its rows' start and count (0: none, or few enough for kv_split_kernel).
+// The tile of slot `slot`: sequence, its rows' start and count (0: none, or few enough for split_part).
 __device__ __forceinline__ int tile_of_slot(const KvView& c, const AttnArgs& a, int64_t slot, int& b, int& t0, int& r0) {
     const int G = a.G;
     auto first = [G](int off, int b) { return (int64_t)off * G / kTileRows + b; };
@@ -584,17 +593,22 @@ __device__ __forceinline__ int tile_of_slot(const KvView& c, const AttnArgs& a, 
     return R <= a.few || r >= R ? 0 : (int)min(R - r, (int64_t)kTileRows);
 }
 
+template <int D>
+struct TileLds {
+    uint4v k[2][2][D / 16][64];              // keys: [buffer][32 tokens][16 dimensions][lane]
+    uint4v v[2][4][D / 32][64];              // values: [buffer][16 tokens][32 dimensions][lane]
+};
 template <int D, bool FP8, bool F16>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tile_kernel(KvView c, AttnArgs a, int64_t n_slots,
-                                                                        int32_t splits) {
+__device__ __forceinline__ void tile_part(const KvView& c, const AttnArgs& a, int64_t n_slots, int32_t splits, uint32_t block,
+                                          TileLds<D>& lds) {
     constexpr int ND = D / 64, NK = D / 16, NV = D / 32;
-    __shared__ uint4v lk[2][2][NK][64];      // keys: [buffer][32 tokens][16 dimensions][lane]
-    __shared__ uint4v lv[2][4][NV][64];      // values: [buffer][16 tokens][32 dimensions][lane]
+    auto& lk = lds.k;
+    auto& lv = lds.v;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, hi = lane >> 5;
-    const int h = blockIdx.x % c.H;
-    const int sp = (int)((blockIdx.x / c.H) % splits);
-    const int64_t slot = n_slots - 1 - blockIdx.x / c.H / splits;     // a sequence's last rows see most: first
+    const int h = block % c.H;
+    const int sp = (int)((block / c.H) % splits);
+    const int64_t slot = n_slots - 1 - block / c.H / splits;     // a sequence's last rows see most: first
     int b, t0, r0;
     const int rows = tile_of_slot(c, a, slot, b, t0, r0);
     if (rows == 0) return;
@@ -858,11 +872,34 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tile_kernel(KvView c
             for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    *reinterpret_cast<float4v*>(a.part_o + at * D + dt * 64 + k * 32 + hi * 16 + i * 4) =
+                    *reinterpret_cast<float4v*>(a.tile_o + at * D + dt * 64 + k * 32 + hi * 16 + i * 4) =
                         float4v{o[dt * 2][4 * k + i], o[dt * 2][8 + 4 * k + i], o[dt * 2 + 1][4 * k + i],
                                 o[dt * 2 + 1][8 + 4 * k + i]};
-        if (hi == 0) a.part_ml[at] = float2v{m_run, l_run};
+        if (hi == 0) a.tile_ml[at] = float2v{m_run, l_run};
     }
+}
+
+// A launch whose sequences all have few rows, and one of both kinds: the tiles'
+// workgroups first, since they take longest, then the others', which fill the gaps.
+template <int D, bool FP8, bool F16>
+__global__ __launch_bounds__(256, kSplitPerCu<D>) void kv_split_kernel(KvView c, AttnArgs a, bool cut) {
+    __shared__ SplitLds<D> lds;
+    split_part<D, FP8, F16>(c, a, cut, blockIdx.x, gridDim.x, lds);
+}
+
+template <int D, bool FP8, bool F16>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_mixed_kernel(KvView c, AttnArgs a, int64_t n_slots, int32_t splits,
+                                                                         bool cut) {
+    __shared__ union Lds {
+        TileLds<D> tile;
+        SplitLds<D> split;
+        __device__ Lds() {}
+    } lds;
+    const uint32_t tiles = (uint32_t)(n_slots * c.H * splits);
+    if (blockIdx.x < tiles)
+        tile_part<D, FP8, F16>(c, a, n_slots, splits, blockIdx.x, lds.tile);
+    else
+        split_part<D, FP8, F16>(c, a, cut, blockIdx.x - tiles, gridDim.x - tiles, lds.split);
 }
 
 // Adds the partial sums of a tile's shares in their order: a workgroup for each
@@ -881,13 +918,13 @@ __global__ __launch_bounds__(256) void kv_tile_join_kernel(KvView c, AttnArgs a,
     float m = kNoMax, l = 0.0f, v[D / 32] = {};
     for (int sp = 0; sp < shares; ++sp) {
         const int64_t at = ((slot * c.H + h) * splits + sp) * kTileRows + i;
-        const float2v p = a.part_ml[at];
+        const float2v p = a.tile_ml[at];
         const float m2 = fmaxf(m, p.x);
         const float f = __builtin_amdgcn_exp2f(m - m2), e = __builtin_amdgcn_exp2f(p.x - m2);
         m = m2;
         l = l * f + p.y * e;
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k) v[k] = v[k] * f + a.part_o[at * D + d0 + k] * e;
+        for (int k = 0; k < D / 32; ++k) v[k] = v[k] * f + a.tile_o[at * D + d0 + k] * e;
     }
     const float norm = l > 0.0f ? 1.0f / l : 0.0f;
     const int row = r0 + i;
@@ -896,15 +933,20 @@ __global__ __launch_bounds__(256) void kv_tile_join_kernel(KvView c, AttnArgs a,
     for (int k = 0; k < D / 32; k += 2) *reinterpret_cast<uint32_t*>(out + k) = pack2<F16>(v[k] * norm, v[k + 1] * norm);
 }
 
-// Shares of a tile: enough workgroups for two on every compute unit, where the workspace holds their sums.
-int tile_splits(const KvView& c, int64_t slots, int n_cu, int64_t room) {
-    const int64_t tiles = slots * c.H, one = tiles * kTileRows * (c.D + 2) * 4;
+// Shares of a tile: enough workgroups for two on every compute unit, where the
+// workspace holds their sums.  Which sequences have many rows is known on the
+// device only; of k of them, at most max_new tokens each and the others one, k is
+// put at 1.5 times its least.
+int tile_splits(const KvView& c, const AttnArgs& a, int64_t slots, int n_cu, int64_t room) {
+    const int64_t one = slots * c.H * kTileRows * (c.D + 2) * 4;
+    const int64_t k = std::min<int64_t>(c.B, 3 * (int64_t)std::max(c.T - c.B, 0) / (2 * std::max(c.max_new - 1, 1)) + 1);
+    const int64_t tiles = std::max(k, (int64_t)c.T * a.G / kTileRows + k / 2) * c.H;
     return (int)std::max<int64_t>(1, std::min<int64_t>({(2 * (int64_t)n_cu + tiles - 1) / tiles, room / one, 64}));
 }
 
 }  // namespace
 
-// The counts of a new workspace (kv_split_kernel leaves them at zero).
+// The counts of a new workspace (the last of a segment's parts leaves them at zero).
 __global__ void kv_clear_kernel(uint32_t* p, int n) {
     for (int i = threadIdx.x; i < n; i += blockDim.x) p[i] = 0;
 }
@@ -927,43 +969,38 @@ hipError_t launch_kv_attention(const KvView& c, const void* q, int64_t q_stride,
     a.window = window;
     a.sinks = sinks;
     a.few = kFewRows;
-    // kv_split_kernel's workspace, then the tiles' (they run one after the other on the same memory)
     WsCarve ws{(char*)workspace, (size_t)workspace_bytes};
     a.arrived = ws.take<uint32_t>(kMaxParts * 2);
-    const size_t head = ws.off;
     // as many parts as workgroups fit the device, and 2.5 for each segment where that is more; segments stay whole
-    // where the workspace does not hold that many parts
-    const int64_t segments = (int64_t)c.B * c.H, fit = (int64_t)n_cu * (c.D == 64 ? kSplitPerCu<64> : c.D == 128 ? kSplitPerCu<128> : kSplitPerCu<256>);
-    const int64_t room = std::min<int64_t>((workspace_bytes - (int64_t)head - 4096) / (kFewRows * (c.D + 2) * 4), kMaxParts);
+    // where half the workspace does not hold that many parts
+    const int64_t segments = (int64_t)c.B * c.H;
+    const int64_t fit = (int64_t)n_cu * (c.D == 64 ? kSplitPerCu<64> : c.D == 128 ? kSplitPerCu<128> : kSplitPerCu<256>);
+    const int64_t room = std::min<int64_t>(workspace_bytes / 2 / (kFewRows * (c.D + 2) * 4), kMaxParts);
     const bool cut = segments * 3 <= room * 2;
     const int64_t wgs = cut ? std::min(std::max(fit, segments * 5 / 2), room) : segments;
-    if (wgs >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
     if (cut) {
         a.part_ml = ws.take<float2v>(wgs * kFewRows);
         a.part_o = ws.take<float>(wgs * kFewRows * c.D);
     }
     const int64_t slots = (int64_t)c.T * a.G / kTileRows + c.B;
-    if (!ws.ok()) return hipErrorInvalidConfiguration;
     const bool tiles = (int64_t)c.max_new * a.G > a.few;
-    const int splits = tiles ? tile_splits(c, slots, n_cu, workspace_bytes - (int64_t)head - 4096) : 1;
-    if (tiles && slots * c.H * std::max(splits, kTileRows / 8) >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
+    const int splits = tiles ? tile_splits(c, a, slots, n_cu, workspace_bytes - (int64_t)ws.off - 4096) : 1;
+    const int64_t tile_wgs = tiles ? slots * c.H * splits : 0, joiners = splits > 1 ? slots * c.H * (kTileRows / 8) : 0;
+    if (splits > 1) {
+        a.tile_ml = ws.take<float2v>(tile_wgs * kTileRows);
+        a.tile_o = ws.take<float>(tile_wgs * kTileRows * c.D);
+    }
+    if (!ws.ok() || wgs + tile_wgs >= (int64_t)1 << 24 || joiners >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
     return by_types(c, [&](auto fp8, auto f16) {
         auto run = [&](auto d) {
             constexpr int D = decltype(d)::value;
-            kv_split_kernel<D, fp8.value, f16.value><<<(uint32_t)wgs, 256, 0, s>>>(c, a, cut);
-            if (tiles) {
-                AttnArgs t = a;
-                WsCarve w{(char*)workspace, (size_t)workspace_bytes, head};
-                if (splits > 1) {
-                    t.part_ml = w.take<float2v>(slots * c.H * splits * kTileRows);
-                    t.part_o = w.take<float>(slots * c.H * splits * kTileRows * D);
-                }
-                kv_tile_kernel<D, fp8.value, f16.value>
-                    <<<(uint32_t)(slots * c.H * splits), 256, 0, s>>>(c, t, slots, splits);
-                if (splits > 1)
-                    kv_tile_join_kernel<D, f16.value>
-                        <<<(uint32_t)(slots * c.H * (kTileRows / 8)), 256, 0, s>>>(c, t, splits);
-            }
+            if (tiles)
+                kv_mixed_kernel<D, fp8.value, f16.value>
+                    <<<(uint32_t)(tile_wgs + wgs), 256, 0, s>>>(c, a, slots, splits, cut);
+            else
+                kv_split_kernel<D, fp8.value, f16.value><<<(uint32_t)wgs, 256, 0, s>>>(c, a, cut);
+            if (joiners)
+                kv_tile_join_kernel<D, f16.value><<<(uint32_t)joiners, 256, 0, s>>>(c, a, splits);
             return hipGetLastError();
         };
         if (c.D == 64) return run(std::integral_constant<int, 64>{});
