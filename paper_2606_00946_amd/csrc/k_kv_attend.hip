@@ -112,7 +112,6 @@ constexpr int kMinUnits = 8;        // no segment is cut finer
 constexpr float kNoMax = -1e30f;     // running maximum of nothing
 constexpr float kTop = 7.0f;         // weights start below 2^7 ...
 constexpr float kMostWeight = 0x1p+15f; // of the sum of a lane's weights, before the maximum moves
-constexpr float kGrow = 8.0f;        // ... and the maximum moves when one would pass 2^15
 
 // A sequence of the call as split_part sees it; units of one kv head, 0: too many rows for it.
 struct Seq {
@@ -273,7 +272,7 @@ __device__ __forceinline__ void add_parts(const AttnArgs& a, uint32_t first, int
 // sums, which the last workgroup to finish adds.  A wave takes 32 of a unit's 128
 // tokens at a time: scores transposed (tokens x rows), so that their registers are
 // the second operand of the product with the values as they stand; codes go from
-// memory to registers in 16-byte loads, one step ahead of their use.
+// memory to registers in 16-byte loads, two steps ahead of their use.
 template <int D>
 struct SplitLds {
     float comb[4][16][D + 4];
@@ -291,12 +290,14 @@ __device__ __forceinline__ void split_part(const KvView& c, const AttnArgs& a, b
     // Segments are cut into equal parts of at most `most` units, so that about as many parts as workgroups hold all units and a
     // long sequence weighs no more on one workgroup than its share (not cut: a part is a segment, found at once).
     uint32_t most = ~0u;
+    Seq mine;                            // of the first 64 sequences, a lane each
     if (cut) {
-        uint64_t total = 0;
-        for (int b = lane; b < c.B; b += 64) total += seq_of(c, a, b).units;
-#pragma unroll
-        for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o);
-        const uint64_t all = (uint64_t)uniform((int64_t)total) * c.H;
+        mine.units = 0;
+        if (lane < c.B) mine = seq_of(c, a, lane);
+        uint64_t all = __builtin_amdgcn_readlane(wave_scan((uint32_t)mine.units), 63);      // below 2^23 each
+        for (int b0 = 64; b0 < c.B; b0 += 64)
+            all += __builtin_amdgcn_readlane(wave_scan(b0 + lane < c.B ? (uint32_t)seq_of(c, a, b0 + lane).units : 0u), 63);
+        all *= (uint32_t)c.H;
         const uint32_t room = blocks_ - (uint32_t)(c.B * c.H);
         // 2^24 units and more, the largest segment, cut nothing
         const uint64_t each = all >> 31 ? (all + room - 1) / room : ((uint32_t)all + room - 1) / room;
@@ -308,22 +309,17 @@ __device__ __forceinline__ void split_part(const KvView& c, const AttnArgs& a, b
         uint32_t seg = part;             // first part of the segment
         if (cut) {
             // sequences' first parts are the sums of the parts before them
-            uint32_t base = 0;
-            int b0 = 0;
-            Seq mine;
+            uint32_t base = 0, own = 0, end = 0;
             uint64_t m = 0;
-            uint32_t own = 0, end = 0;
+            Seq its = mine;
+            int b0 = 0;
             for (; b0 < c.B; b0 += 64) {
-                mine.units = 0;
-                if (b0 + lane < c.B) mine = seq_of(c, a, b0 + lane);
-                own = ((uint32_t)mine.units + most - 1) / most;
-                end = own * (uint32_t)c.H;           // inclusive sums
-#pragma unroll
-                for (int o = 1; o < 64; o <<= 1) {
-                    const uint32_t v = __shfl_up(end, o);
-                    if (lane >= o) end += v;
+                if (b0 > 0) {
+                    its.units = 0;
+                    if (b0 + lane < c.B) its = seq_of(c, a, b0 + lane);
                 }
-                end += base;
+                own = ((uint32_t)its.units + most - 1) / most;
+                end = base + wave_scan(own * (uint32_t)c.H);
                 m = __ballot(end > part);
                 if (m) break;
                 base = __builtin_amdgcn_readlane(end, 63);
@@ -331,10 +327,10 @@ __device__ __forceinline__ void split_part(const KvView& c, const AttnArgs& a, b
             if (!m) return;
             const int k = __ffsll((long long)m) - 1;
             b = b0 + k;
-            seq.t0 = __builtin_amdgcn_readlane(mine.t0, k);
-            seq.n = __builtin_amdgcn_readlane(mine.n, k);
-            seq.past = __builtin_amdgcn_readlane(mine.past, k);
-            seq.units = __builtin_amdgcn_readlane(mine.units, k);
+            seq.t0 = __builtin_amdgcn_readlane(its.t0, k);
+            seq.n = __builtin_amdgcn_readlane(its.n, k);
+            seq.past = __builtin_amdgcn_readlane(its.past, k);
+            seq.units = __builtin_amdgcn_readlane(its.units, k);
             pieces = __builtin_amdgcn_readlane(own, k);
             const uint32_t start = __builtin_amdgcn_readlane(end, k) - (uint32_t)pieces * c.H;
             h = (int)((part - start) / (uint32_t)pieces);
@@ -358,136 +354,158 @@ __device__ __forceinline__ void split_part(const KvView& c, const AttnArgs& a, b
         const int32_t pos = past + col / a.G;                // the column's position
         const int32_t pos_last = past + n - 1;
 
-        half8 q[ND][2];
-        const float undo = load_queries<D, F16>(a, h, t0, col, rows, q);
-        const float s2 = a.scale2 * undo;
-
-        // step i's two blocks
+        // A wave's blocks, two a step: their pages and scales 32 steps at a time, lane 2 i + e holding block e of step i.
         const Blocks blocks(c, b, h);
         const int steps = u1 - u0;
-        struct Meta { int32_t page[2]; float ks[2], vs[2]; };
         auto tile_of = [&](int i, int e) { return (u0 + i) * kUnit + wave * 2 + e; };
-        auto find_page = [&](int i, Meta& m) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) m.page[e] = blocks.page(span.tile(tile_of(i, e)), (i < steps) & (tile_of(i, e) < span.n));
+        auto load_pages = [&](int i0) {
+            return blocks.pages[min(span.tile(tile_of(i0 + (lane >> 1), lane & 1)), blocks.n_blocks - 1) >> blocks.shift];
         };
-        auto find_scales = [&](Meta& m) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                m.ks[e] = blocks.scale(blocks.ks, m.page[e]);
-                m.vs[e] = blocks.scale(blocks.vs, m.page[e]);
-            }
+        auto checked = [&](int32_t page, int i0) {
+            const int i = i0 + (lane >> 1);
+            const bool there = (i < steps) & (tile_of(i, lane & 1) < span.n) & ((uint32_t)page < (uint32_t)blocks.n_pages);
+            return there ? page : -1;
         };
+        auto load_scale = [&](const float* p, int32_t page) {
+            return page >= 0 ? p[(int64_t)page * blocks.H] : 1.0f;
+        };
+        auto of_lane = [](float x, int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l)); };
+        const int32_t first_pages = load_pages(0);
+        int32_t later = load_pages(32);
+
+        half8 q[ND][2];
+        const float s2 = a.scale2 * load_queries<D, F16>(a, h, t0, col, rows, q);
+
+        // blocks (of the span) that all rows see whole, but for the sinks
+        const int32_t base_i = span.n_sink - span.win;
+        const int32_t full_lo = a.window > 0 ? max(span.n_sink, ((pos_last - a.window + 16) >> 4) + base_i) : 0;
+        const int32_t full_hi = ((past - 15) >> 4) + base_i;
+
         struct Raw { uint4v k[2][ND], v[2][ND]; };
-        // (of page 0 for an absent block: hidden from the sums)
-        auto fetch = [&](int i, const Meta& m, const uint8_t* codes, uint32_t lane_at, uint4v (&r)[2][ND]) {
+        // codes of step i (of page 0 for an absent block: hidden from the sums)
+        auto fetch = [&](int i, int32_t pages, const uint8_t* codes, uint32_t lane_at, uint4v (&r)[2][ND]) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const uint8_t* p = codes + blocks.at(m.page[e], span.tile(tile_of(i, e))) + lane_at;
+                const int32_t page = __builtin_amdgcn_readlane(pages, (i & 31) * 2 + e);
+                const uint8_t* p = codes + blocks.at(page, span.tile(tile_of(i, e)));
 #pragma unroll
-                for (int dt = 0; dt < ND; ++dt) r[e][dt] = *reinterpret_cast<const uint4v*>(p + dt * 1024);
+                for (int dt = 0; dt < ND; ++dt) r[e][dt] = *reinterpret_cast<const uint4v*>(p + lane_at + dt * 1024);
             }
         };
-        auto fetch_k = [&](int i, const Meta& m, Raw& r) { fetch(i, m, blocks.k, col * 64 + g * 16, r.k); };
-        auto fetch_v = [&](int i, const Meta& m, Raw& r) { fetch(i, m, blocks.v, lane * 16, r.v); };
+        auto fetch_k = [&](int i, int32_t pages, Raw& r) { fetch(i, pages, blocks.k, col * 64 + g * 16, r.k); };
+        auto fetch_v = [&](int i, int32_t pages, Raw& r) { fetch(i, pages, blocks.v, lane * 16, r.v); };
         float m_run = kNoMax, l_run = 0.0f;
         float4v o[ND][4] = {};
-        // One step.
-        auto step = [&](int i, const Meta& m, Raw& r) {
+        // pages of the steps whose codes are fetched; of those that are computed, with their scales
+        int32_t ahead = checked(first_pages, 0), pages = ahead, pages_next = -1;
+        float ks = load_scale(blocks.ks, pages), vs = load_scale(blocks.vs, pages), ks_next = 1.0f, vs_next = 1.0f;
+        // One step; the codes of step i + 2 go into the registers that it has read.
+        auto step = [&](int i, Raw& r) {
             float4v s[2] = {};
-            {
 #pragma unroll
-                for (int dt = 0; dt < ND; ++dt)
+            for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-                    for (int k = 0; k < 2; ++k)
+                for (int k = 0; k < 2; ++k)
 #pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            s[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-                                code_halves8<FP8>(r.k[e][dt][2 * k], r.k[e][dt][2 * k + 1]), q[dt][k], s[e], 0, 0, 0);
+                    for (int e = 0; e < 2; ++e)
+                        s[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                            code_halves8<FP8>(r.k[e][dt][2 * k], r.k[e][dt][2 * k + 1]), q[dt][k], s[e], 0, 0, 0);
+            fetch_k(i + 2, ahead, r);
+            float f[2], lv[2], iv[2];
+            const int i0 = tile_of(i, 0);
+            int32_t there[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int l = (i & 31) * 2 + e;
+                there[e] = __builtin_amdgcn_readlane(pages, l);
+                const float b = of_lane(vs, l);
+                f[e] = of_lane(ks, l) * s2;
+                lv[e] = __builtin_amdgcn_logf(b);
+                iv[e] = __builtin_amdgcn_rcpf(b);
             }
-            {
-                float x[2][4], f[2], lv[2], iv[2];
-                int32_t tok[2];
-                bool all = true;
+            float x[2][4];
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[e][k] = fmaf(s[e][k], f[e], lv[e]);
+            if (((there[0] | there[1]) < 0) | (i0 < full_lo) | (i0 + 1 > full_hi)) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    f[e] = m.ks[e] * s2;
-                    lv[e] = __builtin_amdgcn_logf(m.vs[e]);
-                    iv[e] = __builtin_amdgcn_rcpf(m.vs[e]);
-                    tok[e] = span.tile(tile_of(i, e)) * 16;
-                    all &= (m.page[e] >= 0) & (tok[e] + 15 <= past) &
-                           ((a.window == 0) | (tok[e] > pos_last - a.window) | (tok[e] + 15 < a.sinks));
+                    const int32_t tok = span.tile(i0 + e) * 16;
+                    const Sight see = sight(a, there[e], pos, tok);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) x[e][k] = see.sees(4 * g + k) ? x[e][k] : -INFINITY;
+                    // codes of nobody's tokens may be NaN: out of the product
+                    const int32_t left = there[e] >= 0 ? end_tok - (tok + 4 * g) : 0;
+                    const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
+#pragma unroll
+                    for (int dt = 0; dt < ND; ++dt) r.v[e][dt] &= keep;
                 }
+            }
+            half8 p;
+            float sum[2];
+            auto weigh = [&] {
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
+                for (int e = 0; e < 2; ++e) {
+                    float w[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) x[e][k] = fmaf(s[e][k], f[e], lv[e]);
-                if (!all) {
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const Sight see = sight(a, m.page[e], pos, tok[e]);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) x[e][k] = see.sees(4 * g + k) ? x[e][k] : -INFINITY;
-                        // codes of nobody's tokens may be NaN: out of the product
-                        const int32_t left = m.page[e] >= 0 ? end_tok - (tok[e] + 4 * g) : 0;
-                        const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
-#pragma unroll
-                        for (int dt = 0; dt < ND; ++dt) r.v[e][dt] &= keep;
+                    for (int k = 0; k < 4; ++k) {
+                        w[k] = __builtin_amdgcn_exp2f(x[e][k] - (m_run - kTop));
+                        p[4 * e + k] = (_Float16)w[k];
                     }
+                    sum[e] = (w[0] + w[1]) + (w[2] + w[3]);
                 }
+            };
+            weigh();
+            // where a sum shows that a weight may not fit a half, the maximum moves first
+            if (__any(sum[0] + sum[1] > kMostWeight)) {
                 float mx = -INFINITY;
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) mx = fmaxf(mx, x[e][k]);
-                if (__any(mx > m_run + kGrow)) {
-                    mx = fmaxf(mx, __shfl_xor(mx, 16));
-                    mx = fmaxf(mx, __shfl_xor(mx, 32));
-                    const float top = fmaxf(m_run, mx);
-                    const float f = __builtin_amdgcn_exp2f(m_run - top);
-                    m_run = top;
-                    l_run *= f;
-#pragma unroll
-                    for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) o[dt][k] *= f;
-                }
-                half8 p;
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    float w[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) w[k] = __builtin_amdgcn_exp2f(x[e][k] - (m_run - kTop));
-                    l_run = fmaf((w[0] + w[1]) + (w[2] + w[3]), iv[e], l_run);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) p[4 * e + k] = (_Float16)w[k];
-                }
+                mx = fmaxf(mx, __shfl_xor(mx, 16));
+                mx = fmaxf(mx, __shfl_xor(mx, 32));
+                const float top = fmaxf(m_run, mx);
+                const float down = __builtin_amdgcn_exp2f(m_run - top);
+                m_run = top;
+                l_run *= down;
 #pragma unroll
                 for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        o[dt][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-                            code_halves8<FP8>(r.v[0][dt][k], r.v[1][dt][k]), p, o[dt][k], 0, 0, 0);
+                    for (int k = 0; k < 4; ++k) o[dt][k] *= down;
+                weigh();
             }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) l_run = fmaf(sum[e], iv[e], l_run);
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    o[dt][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(code_halves8<FP8>(r.v[0][dt][k], r.v[1][dt][k]), p,
+                                                                      o[dt][k], 0, 0, 0);
+            fetch_v(i + 2, ahead, r);
         };
-
-        // pages are looked up two steps ahead, codes and scales fetched one
-        Meta m0, m1, m2;
         Raw r0, r1;
-        find_page(0, m0);
-        find_page(1, m1);
-        find_scales(m0);
-        fetch_k(0, m0, r0);
-        fetch_v(0, m0, r0);
-        for (int i = 0; i < steps; ++i) {
-            find_page(i + 2, m2);
-            find_scales(m1);
-            fetch_k(i + 1, m1, r1);
-            fetch_v(i + 1, m1, r1);
-            step(i, m0, r0);
-            m0 = m1;
-            m1 = m2;
-            r0 = r1;
+        fetch_k(0, ahead, r0);
+        fetch_v(0, ahead, r0);
+        fetch_k(1, ahead, r1);
+        fetch_v(1, ahead, r1);
+        for (int i = 0; i < steps; i += 2) {
+            if (((i + 2) & 31) == 0) {
+                ahead = checked(later, i + 2);
+                later = load_pages(i + 34);
+                pages_next = ahead;
+                ks_next = load_scale(blocks.ks, ahead);
+                vs_next = load_scale(blocks.vs, ahead);
+            }
+            if (i > 0 && (i & 31) == 0) {
+                pages = pages_next;
+                ks = ks_next;
+                vs = vs_next;
+            }
+            step(i, r0);
+            step(i + 1, r1);
         }
 
         // the four waves' sums
