@@ -676,7 +676,6 @@ __device__ __forceinline__ void tile_part(const KvView& c, const AttnArgs& a, in
             s2 *= half_range_undo(top);
         }
     }
-    s2 = fmaxf(s2, 1e-30f);          // a hidden token's score stays -inf under it
 
     // Blocks (of the span) that all of the wave's rows see whole, but for the sinks, and that any row sees.
     const int32_t base_i = span.n_sink - span.win;
@@ -804,7 +803,7 @@ __device__ __forceinline__ void tile_part(const KvView& c, const AttnArgs& a, in
             }
         };
 #pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = of_lane(scale, e) * s2;
+        for (int e = 0; e < 4; ++e) f[e] = fmaxf(of_lane(scale, e) * s2, 1e-37f);      // not 0: -inf of a hidden token stays
         weigh();
         // weights under the maximum so far; where their sum shows that one may not fit a half, the maximum moves first
         if (__any((sum[0] + sum[1]) + (sum[2] + sum[3]) > kMostWeight)) {

@@ -174,6 +174,29 @@ def test_large_logits_and_values(ctx):
     check_attention(ctx, s, 4, scale=0.02)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("scale", [None, 0.0, 1e-38, -0.1])
+def test_zero_queries_and_keys(ctx, kind, scale):
+    """Padding rows: queries and whole blocks of keys of zeros (whose scale is the least) weigh all tokens alike."""
+    import torch
+    s = Setup([(0, 200), (40, 1), (70, 90), (0, 1)], kind=kind, seed=21)
+    keys, scales = s.bufs[0].view(s.n_pages, -1), s.bufs[2].view(s.n_pages, -1)
+    for b in range(3):
+        pages = torch.from_numpy(s.table[b, :5:2].copy()).cuda()
+        keys[pages[pages >= 0]], scales[pages[pages >= 0]] = 0, 2.0 ** -64
+    tensor = s.tensor
+
+    def some_zero(heads, *a):
+        q = tensor(heads, *a)
+        q[::3] = 0
+        q[1::3, 0] *= 2.0 ** -60
+        return q
+    s.tensor = some_zero
+    note(f"kv zero queries and keys {kind} scale={scale}")
+    check_attention(ctx, s, 4, scale=scale)
+    check_attention(ctx, s, 4, window=50, sinks=3, scale=scale)
+
+
 def test_strides_and_shared_pages(ctx):
     import torch
     s = Setup([(100, 1), (100, 60), (100, 1)], seed=4)
