@@ -522,7 +522,8 @@ int ls_swap_model(ls_ctx* ctx, void* serve_stream, void* train_stream);
  *                inside, tiles of 1,024 bytes in the order [page_tokens / 16][head_dim / 64],
  *                a tile being [16 tokens][64 dims] for k and [4][64 dims][4 tokens] for v.
  *   k_scale, v_scale  fp32 [n_pages x n_kv_heads]: one scale for each page and head;
- *                a code c stands for c * scale.
+ *                a code c stands for c * scale (attention takes a scale below 2^-64, as of a page of
+ *                zeros that no append has opened, for 2^-64).
  * ls_kv_batch  the sequences of a call and their new tokens (host struct of device arrays):
  *   n_seqs, n_tokens, pages_stride, max_new   host values, n_tokens and pages_stride * page_tokens up to 2^30;
  *                max_new bounds any sequence's new tokens

@@ -367,7 +367,7 @@ __device__ __forceinline__ void split_part(const KvView& c, const AttnArgs& a, b
             return there ? page : -1;
         };
         auto load_scale = [&](const float* p, int32_t page) {
-            return page >= 0 ? p[(int64_t)page * blocks.H] : 1.0f;
+            return page >= 0 ? fmaxf(p[(int64_t)page * blocks.H], kScaleMin) : 1.0f;
         };
         auto of_lane = [](float x, int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l)); };
         const int32_t first_pages = load_pages(0);
@@ -749,7 +749,7 @@ __device__ __forceinline__ void tile_part(const KvView& c, const AttnArgs& a, in
         const uint32_t have = (uint32_t)__ballot(pages >= 0) & 15u;
         const int i0 = t * 4, i3 = i0 + 3;
         if ((wrows == 0) | (have == 0) | (i0 > any_hi) | ((i3 < any_lo) & (i0 >= sink_hi))) return;
-        scale = pages >= 0 ? scale : 1.0f;
+        scale = pages >= 0 ? fmaxf(scale, kScaleMin) : 1.0f;
         const float log_scale = __builtin_amdgcn_logf(scale), inv_scale = __builtin_amdgcn_rcpf(scale);
         float16v s[2] = {};
         constexpr int KC = D == 256 ? 4 : NK, VC = D == 256 ? 1 : 2;     // products, and blocks, whose operands are read at once

@@ -197,6 +197,23 @@ def test_zero_queries_and_keys(ctx, kind, scale):
     check_attention(ctx, s, 4, window=50, sinks=3, scale=scale)
 
 
+@pytest.mark.parametrize("fmt", ["fp8", "int8"])
+def test_scales_of_zero(ctx, fmt):
+    """Pages as a new cache holds them, codes and scales zero: tokens whose score and value are 0."""
+    s = Setup([(0, 200), (40, 1), (70, 90), (33, 1)], fmt=fmt, seed=22)
+    for b in range(3):
+        for j in range(0, 5, 2):
+            if 0 <= s.table[b, j] < s.n_pages:
+                for t in s.bufs:
+                    t.view(s.n_pages, -1)[int(s.table[b, j])] = 0
+    for t in s.bufs:
+        t.view(s.n_pages, -1)[s.table[3, :3].tolist()] = 0
+    note(f"kv scales of zero {fmt}")
+    out = check_attention(ctx, s, 4)
+    assert (out[s.off[3]] == 0).all()
+    check_attention(ctx, s, 4, window=30, sinks=5)
+
+
 def test_strides_and_shared_pages(ctx):
     import torch
     s = Setup([(100, 1), (100, 60), (100, 1)], seed=4)
