@@ -554,8 +554,9 @@ int ls_swap_model(ls_ctx* ctx, void* serve_stream, void* train_stream);
  * ls_kv_attention  out row t, head h = sum_j softmax_j(scale q . k_j) v_j over the visible tokens j of the
  *   row's sequence (new ones included: append first), query head h reading kv head
  *   h / (n_q_heads / n_kv_heads).  Token j is visible at position p when j <= p and, with window > 0,
- *   j > p - window or j < sinks.  A row that sees nothing gets 0.  Keys and values that no row of a
- *   16-token block sees are not read; what masked places hold does not reach any result.  Softmax
+ *   j > p - window or j < sinks.  A row that sees nothing gets 0.  What a token
+ *   that no row of the sequence sees holds does not reach any result, NaN codes included; an FP8 cache
+ *   filled otherwise than by ls_kv_append must hold no NaN in a token that some rows see.  Softmax
  *   statistics and sums are fp32; probabilities enter the products in half precision, scaled by a power of two.
  * ls_kv_read  rows of 16-bit keys and values (k_out, v_out, dense) that the cache holds for the batch's
  *   tokens; absent ones read 0.

@@ -157,20 +157,6 @@ __device__ __forceinline__ int seq_of_slot(const KvView& c, int64_t slot, F firs
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// A value that is the same in every lane, for the compiler too.
-__device__ __forceinline__ int64_t uniform(int64_t x) {
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x);
-    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)x >> 32));
-    return (int64_t)((uint64_t)hi << 32 | lo);
-}
-
-// A value that is the same in every lane, from read-only memory through the scalar cache.
-template <class T>
-__device__ __forceinline__ T uniform_load(const T* p) {
-    using C = const __attribute__((address_space(4))) T;
-    return *(C*)(uintptr_t)p;
-}
-
 // Sums of a lane and those below it.
 __device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
     x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false);    // the row's lane 1, 2, 4, 8 below

@@ -68,9 +68,19 @@ struct Sight {
 __device__ __forceinline__ Sight sight(const AttnArgs& a, int32_t page, int32_t pos, int32_t tok) {
     Sight s;
     s.last = page < 0 ? -1 : pos - tok;
-    s.gone = a.window > 0 ? pos - a.window - tok : -1;
+    s.gone = a.window > 0 ? max(pos - a.window, -1) - tok : -1;
     s.sink = a.sinks - tok;
     return s;
+}
+
+// Bytes of four tokens' value codes, from token `tok` on, that enter the product: those
+// before `end` that some row sees, `lo` being where the window of the first row
+// starts.  The others belong to nobody or are hidden, and may be NaN.
+__device__ __forceinline__ uint32_t first_bytes(int32_t n) { return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1; }
+__device__ __forceinline__ uint32_t kept_bytes(const AttnArgs& a, int32_t tok, int32_t lo, int32_t end) {
+    uint32_t m = first_bytes(end - tok);
+    if (a.window > 0) m &= ~first_bytes(lo - tok) | first_bytes(a.sinks - tok);
+    return m;
 }
 
 // The pages of one sequence and kv head: where a 16-token block of it lies.
@@ -86,18 +96,9 @@ struct Blocks {
         : pages(c.pages + (int64_t)b * c.W), n_blocks(c.limit >> 4), n_pages((int32_t)c.n_pages), shift(c.page_shift - 4),
           mask((c.page >> 4) - 1), page_bytes((int64_t)c.H * c.page * c.D), block_bytes(16 * c.D), H(c.H),
           k(c.k + (int64_t)h * c.page * c.D), v(c.v + (int64_t)h * c.page * c.D), ks(c.ks + h), vs(c.vs + h) {}
-    // Page of block `blk`, or -1; always a load, so that no branch comes between the loads around it.
-    __device__ __forceinline__ int32_t page(int32_t blk, bool wanted) const {
-        const int32_t p = uniform_load(pages + (min(blk, n_blocks - 1) >> shift));
-        return (wanted & ((uint32_t)p < (uint32_t)n_pages)) ? p : -1;
-    }
     // Offset of its codes; of some codes for an absent one.
     __device__ __forceinline__ int64_t at(int32_t page, int32_t blk) const {
         return (int64_t)max(page, 0) * page_bytes + (blk & mask) * block_bytes;
-    }
-    __device__ __forceinline__ float scale(const float* s, int32_t page) const {
-        const float x = uniform_load(s + (int64_t)max(page, 0) * H);
-        return page >= 0 ? x : 1.0f;
     }
 };
 
@@ -435,9 +436,7 @@ __device__ __forceinline__ void split_part(const KvView& c, const AttnArgs& a, b
                     const Sight see = sight(a, there[e], pos, tok);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) x[e][k] = see.sees(4 * g + k) ? x[e][k] : -INFINITY;
-                    // codes of nobody's tokens may be NaN: out of the product
-                    const int32_t left = there[e] >= 0 ? end_tok - (tok + 4 * g) : 0;
-                    const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
+                    const uint32_t keep = there[e] >= 0 ? kept_bytes(a, tok + 4 * g, max(past + 1 - a.window, 0), end_tok) : 0u;
 #pragma unroll
                     for (int dt = 0; dt < ND; ++dt) r.v[e][dt] &= keep;
                 }
@@ -636,7 +635,7 @@ __device__ __forceinline__ void tile_part(const KvView& c, const AttnArgs& a, in
     if (sp >= work.shares) return;
     int n_all, t_;
     seq_rows(c, b, t_, n_all);
-    const int32_t end_tok = min(past + n_all, c.limit);
+    const int32_t end_tok = min(past + n_all, c.limit), lo_tok = max(past + r0 / a.G + 1 - a.window, 0);
 
     // this wave's rows and the positions they span
     const int w0 = wave * 32, wrows = min(max(rows - w0, 0), 32);
@@ -715,9 +714,7 @@ __device__ __forceinline__ void tile_part(const KvView& c, const AttnArgs& a, in
             rk[dt] = *reinterpret_cast<const uint4v*>(kp + k_at + dt * 1024);
             rv[dt] = *reinterpret_cast<const uint4v*>(vp + v_at + dt * 1024);
         }
-        // codes of nobody's tokens may be NaN: out of the product
-        const int32_t left = page >= 0 ? end_tok - (blk * 16 + (lane >> 4) * 4) : 0;
-        keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
+        keep = page >= 0 ? kept_bytes(a, blk * 16 + (lane >> 4) * 4, lo_tok, end_tok) : 0u;
     };
     auto stage = [&](int buf) {
         // keys: lane (token lane % 16, dimensions 16 (lane / 16) ..) holds both halves of a product step's operand

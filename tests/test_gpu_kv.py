@@ -214,6 +214,19 @@ def test_scales_of_zero(ctx, fmt):
     check_attention(ctx, s, 4, window=30, sinks=5)
 
 
+@pytest.mark.parametrize("window,sinks", [(20, 0), (37, 5), (100, 18), (2 ** 31 - 1, 2 ** 31 - 1)])
+def test_nan_behind_the_window(ctx, window, sinks):
+    """NaN codes in tokens that the window hides from every row, beside visible ones of the same block."""
+    s = Setup([(300, 1), (900, 1), (333, 40), (261, 2), (500, 70)], H=1, seed=23)
+    for b, past in enumerate(s.past):
+        for name, buf in zip("kv", s.bufs):
+            codes, o = buf.view(s.n_pages, -1), ko.offsets(s.page, s.D, name == "v")
+            for t in range(sinks, past + 1 - window):
+                codes[int(s.table[b, t // s.page]), o[t % s.page].tolist()] = 0x7F
+    note(f"kv nan behind window={window} sinks={sinks}")
+    check_attention(ctx, s, 8, window, sinks)
+
+
 def test_strides_and_shared_pages(ctx):
     import torch
     s = Setup([(100, 1), (100, 60), (100, 1)], seed=4)
