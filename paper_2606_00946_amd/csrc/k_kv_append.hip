@@ -162,7 +162,7 @@ __device__ __forceinline__ void append_row(const KvView& c, const KvRope& r, con
     const float again = held * inv;
     uint8_t* pages = VALUE ? c.v : c.k;
     // heads whose scale grew: what they hold, one after the other
-    uint64_t grown = __ballot(on && w.row0 > 0 && again != 1.0f && u == 0);
+    uint64_t grown = __ballot(on && w.row0 > 0 && scale > held && u == 0);
     while (grown) {
         const int l = __ffsll((long long)grown) - 1;
         grown &= grown - 1;
@@ -254,7 +254,7 @@ __device__ __forceinline__ void append_page(const KvView& c, const KvRope& r, co
     a = wave_max(a);
     const float scale = fmaxf(scale_of<FP8>(a), held), inv = 1.0f / scale;
     const float again = held * inv;
-    if (w.row0 > 0 && again != 1.0f) regrade_rows<D, FP8, VALUE>(base, w.row0, again);
+    if (w.row0 > 0 && scale > held) regrade_rows<D, FP8, VALUE>(base, w.row0, again);
     for (int blk = b0; blk < b1; ++blk) {
         if (!ONE) (void)load(blk);
 #pragma unroll
