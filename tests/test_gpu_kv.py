@@ -580,3 +580,17 @@ def test_refusals(ctx):
         lodestar.KVCache(4, 2, 128, dtype="int4")
     with pytest.raises(ValueError):
         lodestar.KVBatch(s.batch.new_off, s.batch.past, s.batch.pages[0], 3)
+
+
+def test_serving_example():
+    """The example's loop: pages taken over give what computing the prompts gave, answers go on from there."""
+    import torch
+    from examples import serve_kv
+    note("kv serving example")
+    (cold, warm), (k, v) = serve_kv.main(requests=5, steps=6, system=70, longest=100)
+    assert warm[1] <= 5 * serve_kv.BLOCK < cold[1] and k.shape[0] == 64
+    assert torch.isfinite(k.float()).all() and (v != 0).any()
+    # the same cached codes; the order of sums and their roundings to bf16 differ
+    a, b = cold[2].float(), warm[2].float()
+    assert (a - b).abs().max() <= 2.0 ** -5 * a.abs().max()
+    assert cold[0].shape == warm[0].shape == (5, 6)
