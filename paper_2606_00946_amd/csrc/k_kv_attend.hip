@@ -635,7 +635,7 @@ __device__ __forceinline__ void tile_part(const KvView& c, const AttnArgs& a, in
     if (sp >= work.shares) return;
     int n_all, t_;
     seq_rows(c, b, t_, n_all);
-    const int32_t end_tok = min(past + n_all, c.limit), lo_tok = max(past + r0 / a.G + 1 - a.window, 0);
+    const int32_t end_tok = min(past + n_all, c.limit), lo_tok = a.window > 0 ? max(past + r0 / a.G + 1 - a.window, 0) : 0;
 
     // this wave's rows and the positions they span
     const int w0 = wave * 32, wrows = min(max(rows - w0, 0), 32);
@@ -714,7 +714,8 @@ __device__ __forceinline__ void tile_part(const KvView& c, const AttnArgs& a, in
             rk[dt] = *reinterpret_cast<const uint4v*>(kp + k_at + dt * 1024);
             rv[dt] = *reinterpret_cast<const uint4v*>(vp + v_at + dt * 1024);
         }
-        keep = page >= 0 ? kept_bytes(a, blk * 16 + (lane >> 4) * 4, lo_tok, end_tok) : 0u;
+        const bool whole = (page >= 0) & (blk * 16 >= lo_tok) & (blk * 16 + 16 <= end_tok);
+        keep = whole ? ~0u : page >= 0 ? kept_bytes(a, blk * 16 + (lane >> 4) * 4, lo_tok, end_tok) : 0u;
     };
     auto stage = [&](int buf) {
         // keys: lane (token lane % 16, dimensions 16 (lane / 16) ..) holds both halves of a product step's operand
