@@ -706,7 +706,7 @@ __device__ __forceinline__ void tile_part(const KvView& c, const AttnArgs& a, in
 
     // the wave's share of a step: block `wave` of the four
     uint4v rk[ND], rv[ND];
-    uint32_t keep = 0;
+    int32_t kept = 0;                // block whose value codes are masked by token, -1: none are, -2: all are
     auto fetch = [&](int t, int32_t pages) {
         const int32_t page = __builtin_amdgcn_readlane(pages, wave);
         const int32_t blk = span.tile(t * 4 + wave);
@@ -719,8 +719,8 @@ __device__ __forceinline__ void tile_part(const KvView& c, const AttnArgs& a, in
             rk[dt] = *reinterpret_cast<const uint4v*>(kp + k_at + dt * 1024);
             rv[dt] = *reinterpret_cast<const uint4v*>(vp + v_at + dt * 1024);
         }
-        const bool whole = (page >= 0) & (blk * 16 >= lo_tok) & (blk * 16 + 16 <= end_tok);
-        keep = whole ? ~0u : page >= 0 ? kept_bytes(a, blk * 16 + (lane >> 4) * 4, lo_tok, end_tok) : 0u;
+        const bool whole = (blk * 16 >= lo_tok) & (blk * 16 + 16 <= end_tok);
+        kept = page < 0 ? -2 : whole ? -1 : blk;
     };
     auto stage = [&](int buf) {
         // keys: lane (token lane % 16, dimensions 16 (lane / 16) ..) holds both halves of a product step's operand
@@ -733,9 +733,13 @@ __device__ __forceinline__ void tile_part(const KvView& c, const AttnArgs& a, in
         }
         // values: lanes 32 apart hold token groups g and g + 2 of four dimensions; after the exchange each holds both
         // groups of two dimensions, one operand register set each
+        if (kept != -1) {
+            const uint32_t keep = kept >= 0 ? kept_bytes(a, kept * 16 + (lane >> 4) * 4, lo_tok, end_tok) : 0u;
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) rv[dt] &= keep;
+        }
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) {
-            rv[dt] &= keep;
             const auto x = __builtin_amdgcn_permlane32_swap(rv[dt][0], rv[dt][2], false, false);
             const auto y = __builtin_amdgcn_permlane32_swap(rv[dt][1], rv[dt][3], false, false);
             uint4v* d = &lv[buf][wave][dt * 2 + hi][((lane >> 4) & 1) * 32 + (lane & 15)];
