@@ -581,7 +581,7 @@ __device__ __forceinline__ void split_part(const KvView& c, const AttnArgs& a, b
 // kv_tile_join_kernel adds their sums.  Measured: prompts of 6.9k and 6.4k tokens, 32
 // query heads of 128: 1.39 to 1.44 ms, 890 to 920 TFLOP/s (a large half-precision
 // product: 1,290), the matrix pipe busy for 45 % of the time; 3 prompts of 64 dimensions
-// under a window of 1,024: 122 us, 481 TFLOP/s.
+// under a window of 1,024: 122 to 125 us, 470 TFLOP/s.
 constexpr int kTileRows = 128;
 
 using float16v = float __attribute__((ext_vector_type(16)));
