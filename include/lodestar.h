@@ -564,9 +564,10 @@ int ls_swap_model(ls_ctx* ctx, void* serve_stream, void* train_stream);
  * All three are asynchronous on `stream`, need neither model nor cache state,
  * validate on the host, and read device arrays only in bounds whatever these hold.
  * ls_kv_attention joins work split along long sequences through a workspace of
- * the context's own of LS_KV_WORKSPACE_BYTES, allocated by its first call: calls on several streams of one context are ordered by the caller,
- * and a call to be captured into a graph is made once before.  n_seqs or
- * n_tokens 0: nothing is done.
+ * the context's own of LS_KV_WORKSPACE_BYTES, allocated by its first call: calls
+ * on several streams of one context are ordered by the caller, and a call to be
+ * captured into a graph is made once before.  n_seqs or n_tokens 0: nothing is
+ * done.
  */
 #define LS_KV_WORKSPACE_BYTES (64u << 20)
 
