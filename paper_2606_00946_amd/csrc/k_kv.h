@@ -15,6 +15,7 @@
 #include <type_traits>
 
 #include "ls_internal.h"
+#include "ls_kv_slots.h"
 
 namespace ls {
 
@@ -126,9 +127,9 @@ __device__ __forceinline__ int64_t block_at(const KvView& c, int64_t page, int h
     return ((page * c.H + h) * c.page + blk * 16) * c.D;
 }
 
-// Page id of the sequence's page j, or -1 (absent, outside the pool, past the table).
+// Page id of the sequence's page j, or -1 (absent, outside the pool, outside the table).
 __device__ __forceinline__ int64_t page_id(const KvView& c, int b, int j) {
-    if (j >= c.W) return -1;
+    if (j < 0 || j >= c.W) return -1;
     const int32_t p = c.pages[(int64_t)b * c.W + j];
     return p >= 0 && p < c.n_pages ? p : -1;
 }
@@ -140,7 +141,8 @@ __device__ __forceinline__ void seq_rows(const KvView& c, int b, int& t0, int& n
 }
 
 // The sequence that owns work slot `slot` when sequence b's slots start at
-// first(off[b], b), non-decreasing in b: a 64-way search by the whole wave.
+// first(off[b], b), non-decreasing in b: a 64-way search by the whole wave.  Slots
+// before sequence 0's first give 0.
 template <class F>
 __device__ __forceinline__ int seq_of_slot(const KvView& c, int64_t slot, F first) {
     const int lane = threadIdx.x & 63;

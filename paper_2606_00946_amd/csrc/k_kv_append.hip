@@ -306,19 +306,19 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvView c, KvRope r, cons
         const int h0 = (int)((w >> 1) % groups) * heads;
         const int64_t slot = (w >> 1) / groups;
         const int sh = c.page_shift;
-        auto first = [sh](int off, int b) { return (int64_t)(off >> sh) + 2 * (int64_t)b; };
+        auto first = [sh](int off, int b) { return block_slot(off, b, sh); };
         const int b = seq_of_slot(c, slot, first);
         int t0, n;
         seq_rows(c, b, t0, n);
         const int64_t past = max(c.past[b], 0);
-        const int64_t j = (past >> sh) + (slot - first(t0, b));      // the page's place in the sequence
+        const BlockRows its = block_rows(slot - first(t0, b), n, past, sh);
         PageWork p;
-        p.pos0 = j << sh;
-        if (p.pos0 >= past + n || j >= c.W) return;
-        p.page = page_id(c, b, (int)j);
-        p.row0 = (int)(max(past, p.pos0) - p.pos0);
-        p.row1 = (int)(min(past + n, p.pos0 + c.page) - p.pos0);
-        if (p.page < 0 || p.row0 >= p.row1) return;
+        p.row0 = its.row0;
+        p.row1 = its.row1;
+        if (p.row0 >= p.row1 || its.j >= c.W) return;
+        p.pos0 = its.j << sh;
+        p.page = page_id(c, b, (int)its.j);
+        if (p.page < 0) return;
         p.stride = value ? v_stride : k_stride;
         p.src = (value ? v : k) + (t0 + (p.pos0 + p.row0 - past)) * p.stride;
         const int hn = min(heads, c.H - h0);
@@ -391,17 +391,17 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvView c, uint16_t* __rest
     const bool value = w & 1;
     const int h = (int)((w >> 1) % (uint32_t)c.H);
     const int64_t slot = (w >> 1) / (uint32_t)c.H;
-    auto first = [](int off, int b) { return (int64_t)(off >> 4) + 2 * (int64_t)b; };
+    auto first = [](int off, int b) { return block_slot(off, b, 4); };
     const int b = seq_of_slot(c, slot, first);
     int t0, n;
     seq_rows(c, b, t0, n);
     const int64_t past = max(c.past[b], 0);
-    const int64_t blk = (past >> 4) + (slot - first(t0, b));
-    const int64_t pos0 = blk << 4;
-    if (pos0 >= past + n) return;
+    const BlockRows its = block_rows(slot - first(t0, b), n, past, 4);
+    const int row0 = its.row0, row1 = its.row1;
+    if (row0 >= row1) return;
+    const int64_t pos0 = its.j << 4;
     const int64_t j = pos0 >> c.page_shift;
     const int64_t page = j < c.W ? page_id(c, b, (int)j) : -1;
-    const int row0 = (int)(max(past, pos0) - pos0), row1 = (int)(min(past + n, pos0 + 16) - pos0);
     const int64_t ld = (int64_t)c.H * c.D;
     uint16_t* out = (value ? v_out : k_out) + (t0 + pos0 - past) * ld + (int64_t)h * c.D;   // row of token pos0
     const float s = page >= 0 ? (value ? c.vs : c.ks)[page * c.H + h] : 0.0f;

@@ -606,13 +606,13 @@ __device__ __forceinline__ TileWork tile_work(const KvView& c, const AttnArgs& a
 // The tile of slot `slot`: sequence, its rows' start and count (0: none, or few enough for split_part).
 __device__ __forceinline__ int tile_of_slot(const KvView& c, const AttnArgs& a, int64_t slot, int& b, int& t0, int& r0) {
     const int G = a.G;
-    auto first = [G](int off, int b) { return (int64_t)off * G / kTileRows + b; };
+    auto first = [G](int off, int b) { return tile_slot(off, b, G, kTileRows); };
     b = seq_of_slot(c, slot, first);
     int n;
     seq_rows(c, b, t0, n);
-    const int64_t R = (int64_t)n * G, r = (slot - first(t0, b)) * kTileRows;
-    r0 = (int)r;
-    return R <= a.few || r >= R ? 0 : (int)min(R - r, (int64_t)kTileRows);
+    const TileRows its = tile_rows(slot - first(t0, b), n, G, kTileRows);
+    r0 = (int)its.r0;
+    return (int64_t)n * G <= a.few ? 0 : its.rows;
 }
 
 template <int D>
