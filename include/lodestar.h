@@ -566,8 +566,8 @@ int ls_swap_model(ls_ctx* ctx, void* serve_stream, void* train_stream);
  * ls_kv_attention joins work split along long sequences through a workspace of
  * the context's own of LS_KV_WORKSPACE_BYTES, allocated by its first call: calls
  * on several streams of one context are ordered by the caller, and a call to be
- * captured into a graph is made once before.  n_seqs or n_tokens 0: nothing is
- * done.
+ * captured into a graph is made once before (a first call on a capturing stream:
+ * LS_ERR_STATE, nothing is recorded).  n_seqs or n_tokens 0: nothing is done.
  */
 #define LS_KV_WORKSPACE_BYTES (64u << 20)
 

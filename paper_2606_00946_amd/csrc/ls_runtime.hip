@@ -1490,6 +1490,13 @@ int ls_kv_attention(ls_ctx* c, const ls_kv_cache* cache, const ls_kv_batch* batc
     if (!dev.ok) return fail(c, LS_ERR_DEVICE, "cannot select device %d", c->device);
     hipStream_t s = (hipStream_t)stream;
     if (!c->kv_ws_ready) {
+        // a capture would record the allocation and the clearing instead: the memory would be the graph's, the counts not clear
+        hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+        const hipError_t e = hipStreamIsCapturing(s, &capture);
+        if (e != hipSuccess) (void)hipGetLastError();
+        if (e != hipSuccess || capture != hipStreamCaptureStatusNone)
+            return fail(c, LS_ERR_STATE, "a context's first ls_kv_attention allocates its workspace: make one call before "
+                                         "capturing");
         if ((rc = grow(c, &c->kv_ws, &c->kv_ws_cap, LS_KV_WORKSPACE_BYTES, s))) return rc;
         LS_HIP(c, ls::launch_kv_workspace_init(c->kv_ws, s));
         c->kv_ws_ready = true;

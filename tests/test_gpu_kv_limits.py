@@ -1,5 +1,5 @@
 """The paged 8-bit KV cache's calls where their bounds are reached: offsets that
-leave rows to nobody, against the definitions in 64 bits (kv_oracle) with the
+leave rows to nobody, a first call inside a capture, against the definitions in 64 bits (kv_oracle) with the
 tolerances of test_gpu_kv."""
 import numpy as np
 import pytest
@@ -48,3 +48,36 @@ def test_rows_before_the_first_sequence(ctx, G, head, fmt):  # noqa: F811
     want, mag = ko.attention(after, q.double().cpu().numpy(), off, past, table, s.D ** -0.5)
     got = out.double().cpu().numpy()
     assert (np.abs(got - want)[head:] <= (2.0 ** -8 * np.abs(want) + 2.0 ** -9 * mag + 1e-7)[head:]).all()
+
+
+def test_first_call_inside_a_capture():
+    """A context's first attention call is refused on a capturing stream; after one outside, capture and replays work."""
+    import torch
+    own = lodestar.Context(16, (64, 64))
+    s = Setup([(9000, 1), (40, 1), (2000, 1)], seed=31)
+    q = s.tensor(s.H * 4)
+    out, x = torch.zeros_like(q), torch.zeros(4, device="cuda")
+    note("kv first call inside a capture")
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        x.add_(1.0)
+        with pytest.raises(lodestar.LodestarError) as e:
+            own.ls_kv_attention(s.cache, s.batch, q, out)
+    assert e.value.code == lodestar.LS_ERR_STATE and "capturing" in own.last_error()
+    g.replay()
+    torch.cuda.synchronize()
+    assert (x == 1.0).all() and (out == 0).all()
+    note("kv first call outside")
+    own.ls_kv_attention(s.cache, s.batch, q, out)
+    torch.cuda.synchronize()
+    want = out.clone()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        own.ls_kv_attention(s.cache, s.batch, q, out)
+    for i in range(3):
+        note(f"kv replay {i}")
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    own.close()
