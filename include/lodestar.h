@@ -557,7 +557,9 @@ int ls_swap_model(ls_ctx* ctx, void* serve_stream, void* train_stream);
  *   j > p - window or j < sinks.  A row that sees nothing gets 0.  What a token
  *   that no row of the sequence sees holds does not reach any result, NaN codes included; an FP8 cache
  *   filled otherwise than by ls_kv_append must hold no NaN in a token that some rows see.  Softmax
- *   statistics and sums are fp32; probabilities enter the products in half precision, scaled by a power of two.
+ *   statistics and sums are fp32.  Weights (probability times value scale) enter the products in half
+ *   precision, under a power of two that follows the row along its tokens: 11 bits each, or to 2^-16 of the
+ *   sum of the up to 32 weights that one goes with (2^-11 where the mask hides some of these tokens).
  * ls_kv_read  rows of 16-bit keys and values (k_out, v_out, dense) that the cache holds for the batch's
  *   tokens; absent ones read 0.
  *

@@ -4,13 +4,16 @@
 //
 // With key scale a_j and value scale b_j of token j's page and head, and codes
 // K_j, V_j, the row's weights are carried as w_j = b_j 2^(x_j - m), x_j the
-// base-2 logit, so that the value scales enter through the running maximum of
-// x_j + log2 b_j and V_j stays as stored:
+// base-2 logit, so that the value scales enter through x_j + log2 b_j and V_j stays
+// as stored:
 //   out = sum_j w_j V_j / sum_j (w_j / b_j).
-// w_j is at most 2^15 and enters the product in half precision (11 bits, the
-// rounding of the probabilities); codes and 16-bit queries are exact there, a
-// bf16 query after scaling its row by a power of two.  The maximum, the sums and
-// the products are fp32.
+// m is any reference, not only the maximum.  w_j enters the product in half
+// precision, 11 bits from 2^-14 on; codes and 16-bit queries are exact there, a
+// bf16 query after scaling its row by a power of two.  m therefore follows the
+// weights of the tokens at hand: it moves up before one of them does not fit, and
+// down where all of them are small (a first token that takes nearly all weight and
+// has values near zero must not cost the others their bits).  m, the sums and the
+// products are fp32.
 #include <algorithm>
 
 #include "k_kv.h"
@@ -110,9 +113,31 @@ constexpr int kJoin = 16;            // parts that one workgroup adds
 template <int D>
 constexpr int kSplitPerCu = D == 64 ? 4 : D == 128 ? 2 : 1;
 constexpr int kMinUnits = 8;        // no segment is cut finer
-constexpr float kNoMax = -1e30f;     // running maximum of nothing
-constexpr float kTop = 7.0f;         // weights start below 2^7 ...
-constexpr float kMostWeight = 0x1p+15f; // of the sum of a lane's weights, before the maximum moves
+constexpr float kNoMax = -1e30f;     // reference of nothing
+// log2 of a row's largest weight when the reference moves up to it: all of a lane's tokens of
+// a step (8 and 32) may have it within kMostWeight, and later ones twice and eight times that.
+constexpr float kSplitTop = 12.0f, kTileTop = 8.0f;
+// Bounds of the sum of a lane's weights in a step (8 or 32 tokens), beyond which the reference
+// may move.  No weight is too large for a half; and an error of 2^-25, where a weight has less
+// than 11 bits, is 2^-16 of the sum.  Steps that the mask cuts have lanes with one token or
+// two, often small ones: there it is 2^-11.  Measured against no lower bound: 3 prompts of 64
+// dimensions under a window of 1,024 124 -> 125 to 131 us, a mixed step 61.6 -> 62.7, the
+// others 0 to 2 %.
+constexpr float kMostWeight = 0x1.ffp+15f;
+constexpr float kLeast = -9.0f, kLeastCut = -14.0f;       // log2
+__device__ __forceinline__ bool off_range(float sum, bool cut) {
+    return (sum > kMostWeight) | ((sum < (cut ? 0x1p-14f : 0x1p-9f)) & (sum > 0.0f));
+}
+// Whether all weights of a row in the step are below that, mx being its largest logit and
+// 2^top the weight that the reference m stands for.
+__device__ __forceinline__ bool is_low(float m, float mx, float top, bool cut) {
+    return (mx - m < (cut ? kLeastCut : kLeast) - top) & (mx > -INFINITY);
+}
+// The reference that makes the largest 1, as far as the sums have room, `most` being their largest magnitude.
+__device__ __forceinline__ float lowered(float m, float mx, float top, float most) {
+    const float room = fmaxf(100.0f - __builtin_amdgcn_logf(fmaxf(most, 1.0f)), 0.0f);
+    return fmaxf(mx + top, m - room);
+}
 
 // A sequence of the call as split_part sees it; units of one kv head, 0: too many rows for it.
 struct Seq {
@@ -431,7 +456,8 @@ __device__ __forceinline__ void split_part(const KvView& c, const AttnArgs& a, b
             for (int e = 0; e < 2; ++e)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) x[e][k] = fmaf(s[e][k], f[e], lv[e]);
-            if (((there[0] | there[1]) < 0) | (i0 < full_lo) | (i0 + 1 > full_hi)) {
+            const bool masked = ((there[0] | there[1]) < 0) | (i0 < full_lo) | (i0 + 1 > full_hi);
+            if (masked) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int32_t tok = span.tile(i0 + e) * 16;
@@ -451,15 +477,14 @@ __device__ __forceinline__ void split_part(const KvView& c, const AttnArgs& a, b
                     float w[4];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        w[k] = __builtin_amdgcn_exp2f(x[e][k] - (m_run - kTop));
+                        w[k] = __builtin_amdgcn_exp2f(x[e][k] - (m_run - kSplitTop));
                         p[4 * e + k] = (_Float16)w[k];
                     }
                     sum[e] = (w[0] + w[1]) + (w[2] + w[3]);
                 }
             };
             weigh();
-            // where a sum shows that a weight may not fit a half, the maximum moves first
-            if (__any(sum[0] + sum[1] > kMostWeight)) {
+            if (__any(off_range(sum[0] + sum[1], masked))) {
                 float mx = -INFINITY;
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
@@ -467,14 +492,27 @@ __device__ __forceinline__ void split_part(const KvView& c, const AttnArgs& a, b
                     for (int k = 0; k < 4; ++k) mx = fmaxf(mx, x[e][k]);
                 mx = fmaxf(mx, __shfl_xor(mx, 16));
                 mx = fmaxf(mx, __shfl_xor(mx, 32));
-                const float top = fmaxf(m_run, mx);
-                const float down = __builtin_amdgcn_exp2f(m_run - top);
-                m_run = top;
-                l_run *= down;
+                float to = fmaxf(m_run, mx);
+                const bool low = is_low(m_run, mx, kSplitTop, masked);
+                if (__any(low)) {
+                    float most = l_run;
+#pragma unroll
+                    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(o[dt][k][i]));
+                    most = fmaxf(most, __shfl_xor(most, 16));
+                    most = fmaxf(most, __shfl_xor(most, 32));
+                    to = low ? lowered(m_run, mx, kSplitTop, most) : to;
+                }
+                const float by = __builtin_amdgcn_exp2f(m_run - to);
+                m_run = to;
+                l_run *= by;
 #pragma unroll
                 for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) o[dt][k] *= down;
+                    for (int k = 0; k < 4; ++k) o[dt][k] *= by;
                 weigh();
             }
 #pragma unroll
@@ -783,7 +821,8 @@ __device__ __forceinline__ void tile_part(const KvView& c, const AttnArgs& a, in
         };
         read_values(0);
         __builtin_amdgcn_sched_barrier(0);
-        if ((have != 15u) | (i0 < full_lo) | (i3 > full_hi)) {
+        const bool masked = (have != 15u) | (i0 < full_lo) | (i3 > full_hi);
+        if (masked) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const Sight v = sight(a, have >> e & 1 ? 0 : -1, pos, span.tile(i0 + e) * 16);
@@ -799,7 +838,7 @@ __device__ __forceinline__ void tile_part(const KvView& c, const AttnArgs& a, in
         auto weigh = [&] {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float off = of_lane(log_scale, 4 + e) - (m_run - kTop);
+                const float off = of_lane(log_scale, 4 + e) - (m_run - kTileTop);
                 sum[e] = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -812,8 +851,7 @@ __device__ __forceinline__ void tile_part(const KvView& c, const AttnArgs& a, in
 #pragma unroll
         for (int e = 0; e < 4; ++e) f[e] = fmaxf(of_lane(scale, e) * s2, 1e-37f);      // not 0: -inf of a hidden token stays
         weigh();
-        // weights under the maximum so far; where their sum shows that one may not fit a half, the maximum moves first
-        if (__any((sum[0] + sum[1]) + (sum[2] + sum[3]) > kMostWeight)) {
+        if (__any(off_range((sum[0] + sum[1]) + (sum[2] + sum[3]), masked))) {
             float mx = -INFINITY;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -823,13 +861,25 @@ __device__ __forceinline__ void tile_part(const KvView& c, const AttnArgs& a, in
                 mx = fmaxf(mx, fmaf(top, f[e], of_lane(log_scale, 4 + e)));
             }
             mx = fmaxf(mx, __shfl_xor(mx, 32));
-            const float m2 = fmaxf(m_run, mx);
-            const float r = __builtin_amdgcn_exp2f(m_run - m2);
-            m_run = m2;
-            l_run *= r;
+            float to = fmaxf(m_run, mx);
+            const bool low = is_low(m_run, mx, kTileTop, masked);
+            if (__any(low)) {
+                float most = l_run;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) o[i] *= r;
-            weigh();
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) most = fmaxf(most, fabsf(o[i][k]));
+                most = fmaxf(most, __shfl_xor(most, 32));
+                to = low ? lowered(m_run, mx, kTileTop, most) : to;
+            }
+            if (__any(to != m_run)) {
+                const float by = __builtin_amdgcn_exp2f(m_run - to);
+                m_run = to;
+                l_run *= by;
+#pragma unroll
+                for (int i = 0; i < NV; ++i) o[i] *= by;
+                weigh();
+            }
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) l_run = fmaf(sum[e], of_lane(inv_scale, 4 + e), l_run);

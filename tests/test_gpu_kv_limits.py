@@ -81,3 +81,98 @@ def test_first_call_inside_a_capture():
         torch.cuda.synchronize()
         assert torch.equal(out, want)
     own.close()
+
+
+def attention_f64(s, q, scale, floor=0.0, window=0, sinks=0):
+    """(out, sum p |v|, low) of every row over the tokens it sees, in 64 bits on the GPU.
+
+    low: what is lost where the weights (probability times value scale) of the tokens that may go with the first one are
+    held to `floor` of its own: sum over them of min(p, floor p_0 b_0 / b) |v|.  These are the first 64, and with a
+    window the 64 from where it starts for the earliest of up to 128 rows.
+    """
+    import torch
+    host, G = s.host(), q.shape[1] // s.H
+    qd = q.double()
+    out, mag, low = (torch.zeros(q.shape, dtype=torch.float64, device="cuda") for _ in range(3))
+    for b in range(len(s.past)):
+        n, p0 = int(s.new[b]), int(s.past[b])
+        if n == 0:
+            continue
+        rows = slice(int(s.off[b]), int(s.off[b + 1]))
+        k, v = (torch.from_numpy(host.tokens(name, s.table[b], p0 + n)[0]).cuda() for name in "kv")
+        vs = torch.from_numpy(np.repeat(host.scale["v"][s.table[b, :-(-(p0 + n) // s.page)]], s.page, 0)[:p0 + n]).cuda()
+        j, i = torch.arange(p0 + n, device="cuda")[None], p0 + torch.arange(n, device="cuda")[:, None]
+        hidden, near = j > i, (j < 64).expand(n, -1)
+        if window:
+            hidden, near = hidden | ((j <= i - window) & (j >= sinks)), near | (j <= i - window + 64 + 128)
+        for h in range(q.shape[1]):
+            kh, vh = k[:, h // G].contiguous(), v[:, h // G].contiguous()
+            p = torch.softmax((qd[rows, h] @ kh.T.contiguous() * scale).masked_fill(hidden, -np.inf), 1)
+            out[rows, h], mag[rows, h] = p @ vh, p @ vh.abs()
+            first = p[:, :1] * (floor * vs[0, h // G] / vs[:, h // G])[None]
+            low[rows, h] = torch.minimum(p, first).masked_fill(~near, 0.0) @ vh.abs()
+    return out, mag, low
+
+
+def put_row(s, b, t, name, codes):
+    """Writes one token's codes [H x D] or [D]."""
+    import torch
+    buf, o = s.bufs["kv".index(name)].view(s.n_pages, s.H, -1), ko.offsets(s.page, s.D, name == "v")
+    row = np.broadcast_to(codes, (s.H, s.D)).astype(np.uint8)
+    buf[int(s.table[b, t // s.page]), :, o[t % s.page].tolist()] = torch.from_numpy(row.copy()).cuda()
+
+
+def first_token_takes(ctx, H, G, D, past, new, lift, rest, fmt, kind, window=0, sinks=0):  # noqa: F811
+    """The first token takes about all but `rest` of the weight and its values are zeros: what is left decides the output.
+
+    Tolerance: the output's rounding and 2^-9 of sum p |v|, as in test_gpu_kv; and since the weights of up to 64 tokens
+    enter the products together, in half precision with the largest at 2^8 or more: half of a half's least step,
+    2^-33 of the first token's weight, for each token that goes with it.
+    """
+    import torch
+    s = Setup([(past, new)], H=H, D=D, fmt=fmt, kind=kind, seed=int(past + D), poison=False)
+    scale, N = D ** -0.5, window or past + new // 2
+    # values of one sign and large enough for the output's format
+    k, v = (t.view(torch.uint8) for t in s.bufs[:2])
+    v.copy_(torch.randint(0x40, 0x70, v.shape, device="cuda", dtype=torch.uint8))
+    s.bufs[3].fill_(4.0 if fmt == "fp8" else 8.0)
+    s.bufs[3].view(s.n_pages, H)[int(s.table[0, 0])] *= lift
+    s.bufs[2].fill_(2.0 ** -8 if fmt == "fp8" else 2.0 ** -6)
+    s.bufs[2].view(s.n_pages, H)[int(s.table[0, 0])] = 2.0 ** -6
+    # dimension 0 is the first token's alone: its key is 1 there
+    at = torch.from_numpy(ko.offsets(s.page, D, False)[:, 0].copy()).cuda()
+    k.view(s.n_pages, H, -1)[:, :, at] = 0
+    one = np.zeros(D)
+    one[0] = 0x68 if fmt == "fp8" else 64
+    put_row(s, 0, 0, "k", one)
+    put_row(s, 0, 0, "v", np.zeros(D))
+    q = s.tensor(H * G, 1.0)
+    logits = q[:1, :1].double().cpu().numpy() @ s.host().tokens("k", s.table[0], past)[0][1:, 0].T * scale
+    spread = float(np.log(np.mean(np.exp(logits))))
+    q[:, :, 0] = (np.log(N / rest) + spread) / scale
+    out = torch.empty_like(q)
+    note(f"kv a token without value H={H} G={G} D={D} {past}+{new} rest={rest} {window} {fmt} {kind}")
+    ctx.ls_kv_attention(s.cache, s.batch, q, out, window=window, sinks=sinks)
+    want, mag, low = attention_f64(s, q, scale, 2.0 ** -33, window, sinks)
+    u = 2.0 ** -8 if kind == "bf16" else 2.0 ** -10
+    off = (out.double() - want).abs() - (u * want.abs() + 2.0 ** -9 * mag + low + (2.0 ** -25 if kind == "f16" else 0.0))
+    worst = float(((out.double() - want).abs() / mag).max())
+    print(f"  worst error {worst:.2e} of sum p |v|", flush=True)
+    assert bool(torch.isfinite(out).all())
+    assert float(off.max()) <= 0
+
+
+@pytest.mark.parametrize("fmt,kind", [("fp8", "bf16"), ("int8", "f16")])
+@pytest.mark.parametrize("rest", [1e-2, 1e-4, 1e-5, 1e-7])
+@pytest.mark.parametrize("H,G,D,past,new,lift", [(1, 4, 128, 1000, 1, 1.0), (1, 16, 64, 9000, 1, 64.0), (1, 8, 256, 900, 2, 1.0),
+                                                 (1, 4, 128, 3000, 40, 1.0), (8, 16, 64, 2000, 520, 64.0),
+                                                 (8, 16, 128, 2000, 520, 1.0), (4, 32, 256, 700, 300, 1.0)])
+def test_a_token_without_value_takes_most(ctx, H, G, D, past, new, lift, rest, fmt, kind):  # noqa: F811
+    first_token_takes(ctx, H, G, D, past, new, lift, rest, fmt, kind)
+
+
+@pytest.mark.parametrize("rest", [1e-2, 1e-5, 1e-8])
+@pytest.mark.parametrize("H,G,D,past,new,window,sinks", [(1, 4, 128, 5000, 1, 100, 4), (1, 8, 64, 5000, 2, 1000, 16),
+                                                         (8, 16, 128, 2000, 520, 1000, 4), (8, 16, 64, 2000, 520, 600, 1)])
+def test_a_sink_without_value_takes_most(ctx, H, G, D, past, new, window, sinks, rest):  # noqa: F811
+    first_token_takes(ctx, H, G, D, past, new, 1.0, rest, "int8", "f16", window, sinks)
