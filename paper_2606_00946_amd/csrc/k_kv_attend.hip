@@ -113,7 +113,7 @@ constexpr int kJoin = 16;            // parts that one workgroup adds
 template <int D>
 constexpr int kSplitPerCu = D == 64 ? 4 : D == 128 ? 2 : 1;
 constexpr int kMinUnits = 8;        // no segment is cut finer
-constexpr float kNoMax = -1e30f;     // reference of nothing
+constexpr float kNoMax = -3e38f;     // reference of nothing: below every logit
 // log2 of a row's largest weight when the reference moves up to it: all of a lane's tokens of
 // a step (8 and 32) may have it within kMostWeight, and later ones twice and eight times that.
 constexpr float kSplitTop = 12.0f, kTileTop = 8.0f;
@@ -835,14 +835,17 @@ __device__ __forceinline__ void tile_part(const KvView& c, const AttnArgs& a, in
         }
         float f[4], sum[4];
         half8 p[4];
-        auto weigh = [&] {
+        // from the logits as they are rounded for the reference, or in one operation less: the same while a logit's last
+        // bit is below 1, from 2^24 on too large or small by up to that bit
+        auto weigh = [&](auto rounded) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float off = of_lane(log_scale, 4 + e) - (m_run - kTileTop);
+                const float log = of_lane(log_scale, 4 + e), ref = m_run - kTileTop, off = log - ref;
                 sum[e] = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float w = __builtin_amdgcn_exp2f(fmaf(s[e >> 1][(e & 1) * 8 + i], f[e], off));
+                    const float x = s[e >> 1][(e & 1) * 8 + i];
+                    const float w = __builtin_amdgcn_exp2f(rounded ? fmaf(x, f[e], log) - ref : fmaf(x, f[e], off));
                     sum[e] += w;
                     p[e][i] = (_Float16)w;
                 }
@@ -850,8 +853,9 @@ __device__ __forceinline__ void tile_part(const KvView& c, const AttnArgs& a, in
         };
 #pragma unroll
         for (int e = 0; e < 4; ++e) f[e] = fmaxf(of_lane(scale, e) * s2, 1e-37f);      // not 0: -inf of a hidden token stays
-        weigh();
-        if (__any(off_range((sum[0] + sum[1]) + (sum[2] + sum[3]), masked))) {
+        weigh(std::false_type{});
+        const float level = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        if (__any(off_range(level, masked))) {
             float mx = -INFINITY;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -872,13 +876,13 @@ __device__ __forceinline__ void tile_part(const KvView& c, const AttnArgs& a, in
                 most = fmaxf(most, __shfl_xor(most, 32));
                 to = low ? lowered(m_run, mx, kTileTop, most) : to;
             }
-            if (__any(to != m_run)) {
+            if (__any((to != m_run) | (level > kMostWeight))) {
                 const float by = __builtin_amdgcn_exp2f(m_run - to);
                 m_run = to;
                 l_run *= by;
 #pragma unroll
                 for (int i = 0; i < NV; ++i) o[i] *= by;
-                weigh();
+                weigh(std::true_type{});
             }
         }
 #pragma unroll

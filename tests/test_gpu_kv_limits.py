@@ -7,7 +7,7 @@ import pytest
 import kv_oracle as ko
 from gpu_helpers import note
 from paper_2606_00946_amd import lodestar
-from test_gpu_kv import Setup, ctx  # noqa: F401
+from test_gpu_kv import Setup, check_attention, ctx  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -176,3 +176,38 @@ def test_a_token_without_value_takes_most(ctx, H, G, D, past, new, lift, rest, f
                                                          (8, 16, 128, 2000, 520, 1000, 4), (8, 16, 64, 2000, 520, 600, 1)])
 def test_a_sink_without_value_takes_most(ctx, H, G, D, past, new, window, sinks, rest):  # noqa: F811
     first_token_takes(ctx, H, G, D, past, new, 1.0, rest, "int8", "f16", window, sinks)
+
+
+@pytest.mark.parametrize("kind,log_q,log_scale", [("bf16", 50, 0), ("f16", 15, 20), ("bf16", 4, 0), ("f16", 10, -2)])
+@pytest.mark.parametrize("sign,window", [(-1, 1), (1, 1), (1, 0)])
+@pytest.mark.parametrize("G,seqs", [(4, [(0, 1), (70, 2), (200, 1)]), (8, [(0, 200), (33, 90), (5, 1)])])
+def test_huge_logits(ctx, G, seqs, kind, log_q, log_scale, sign, window):  # noqa: F811
+    """Logits of about 2^27 and 2^115 of either sign: a row with one visible token is that token's value, one with
+    many the largest's."""
+    import torch
+    s = Setup(seqs, kind=kind, seed=51)
+    k = s.bufs[0].view(torch.uint8)
+    k.copy_(torch.randint(0x40, 0x70, k.shape, device="cuda", dtype=torch.uint8))
+    s.bufs[2].fill_(2.0 ** (50 if log_q == 50 else 64 if log_q == 15 else 8))
+    q = torch.full((s.T, s.H * G, s.D), sign * 2.0 ** log_q, dtype=s.kind, device="cuda")
+    s.tensor = lambda *a: q
+    note(f"kv huge logits G={G} {kind} {log_q} {sign} window={window}")
+    check_attention(ctx, s, G, window=window, scale=2.0 ** log_scale)
+
+
+@pytest.mark.parametrize("G,seqs", [(4, [(300, 1), (40, 2), (0, 1)]), (8, [(300, 90), (5, 40), (700, 1)])])
+def test_nan_and_infinite_queries(ctx, G, seqs):  # noqa: F811
+    """A row whose query holds NaN or an infinity does not change the others'."""
+    import torch
+    s = Setup(seqs, seed=52)
+    q = s.tensor(s.H * G)
+    out, clean = torch.empty_like(q), torch.empty_like(q)
+    note(f"kv nan queries G={G}")
+    ctx.ls_kv_attention(s.cache, s.batch, q, clean)
+    bad = torch.zeros(q.shape[:2], dtype=torch.bool, device="cuda")
+    for n, (t, h) in enumerate([(0, 1), (1, 3), (s.T // 2, 2), (s.T - 1, 0)]):
+        q[t, h, 5 * n] = (float("nan"), float("inf"))[n % 2]
+        bad[t, h] = True
+    ctx.ls_kv_attention(s.cache, s.batch, q, out)
+    torch.cuda.synchronize()
+    assert torch.equal(out[~bad], clean[~bad])
