@@ -525,8 +525,8 @@ int ls_swap_model(ls_ctx* ctx, void* serve_stream, void* train_stream);
  *                a code c stands for c * scale (attention takes a scale below 2^-64, as of a page of
  *                zeros that no append has opened, for 2^-64).
  * ls_kv_batch  the sequences of a call and their new tokens (host struct of device arrays):
- *   n_seqs, n_tokens, pages_stride, max_new   host values, n_tokens and pages_stride * page_tokens up to 2^30;
- *                max_new bounds any sequence's new tokens
+ *   n_seqs, n_tokens, pages_stride, max_new   host values, n_tokens below 2^30, pages_stride * page_tokens up to
+ *                2^30; max_new bounds any sequence's new tokens
  *   dtype        of the 16-bit tensors of the call: LS_BF16 or LS_FP16
  *   new_off      int32 [n_seqs + 1], 0 = new_off[0] <= ... <= new_off[n_seqs] = n_tokens: sequence b's
  *                new tokens are rows new_off[b] .. new_off[b+1] of the call's tensors (none: left out)

@@ -112,7 +112,9 @@ constexpr int kJoin = 16;            // parts that one workgroup adds
 // Workgroups of kv_split_kernel on a compute unit, by its registers.
 template <int D>
 constexpr int kSplitPerCu = D == 64 ? 4 : D == 128 ? 2 : 1;
-constexpr int kMinUnits = 8;        // no segment is cut finer
+// Segments of up to this many units stay whole.  4 and 16: 12 windows of 4,096 tokens 19.0 and 19.1 us, 64 decoding
+// sequences 51.0 and 53.5; 8: 16.9 and 50.9.
+constexpr int kMinUnits = 8;
 constexpr float kNoMax = -3e38f;     // reference of nothing: below every logit
 // log2 of a row's largest weight when the reference moves up to it: all of a lane's tokens of
 // a step (8 and 32) may have it within kMostWeight, and later ones twice and eight times that.
@@ -299,8 +301,8 @@ __device__ __forceinline__ void add_parts(const AttnArgs& a, uint32_t first, int
 // tokens at a time: scores transposed (tokens x rows), so that their registers are
 // the second operand of the product with the values as they stand; codes go from
 // memory to registers in 16-byte loads, two steps ahead of their use.  Measured: 64
-// sequences of 105k tokens in all, 8 kv heads of 128: 50.5 us, 4.3 TB/s; 4 sequences of
-// 281k tokens 115 us, 5.0 TB/s (a large copy: 4.8); 1 sequence of 300 tokens 7.8 us.
+// sequences of 105k tokens in all, 8 kv heads of 128: 50.9 us, 4.25 TB/s; 4 sequences of
+// 281k tokens 115 us, 5.0 TB/s (a large copy: 4.8); 1 sequence of 300 tokens 8.0 us.
 template <int D>
 struct SplitLds {
     float comb[4][16][D + 4];
@@ -617,9 +619,9 @@ __device__ __forceinline__ void split_part(const KvView& c, const AttnArgs& a, b
 // (tokens x rows): their registers are the second operand of the product with the
 // values.  Few tiles: `splits` workgroups share a tile's tokens and
 // kv_tile_join_kernel adds their sums.  Measured: prompts of 6.9k and 6.4k tokens, 32
-// query heads of 128: 1.39 to 1.44 ms, 890 to 920 TFLOP/s (a large half-precision
-// product: 1,290), the matrix pipe busy for 45 % of the time; 3 prompts of 64 dimensions
-// under a window of 1,024: 122 to 125 us, 470 TFLOP/s.
+// query heads of 128: 1.34 to 1.45 ms, 880 to 950 TFLOP/s (a large half-precision
+// product: 1,290), the matrix pipe busy for 43 % of the time; 3 prompts of 64 dimensions
+// under a window of 1,024: 125 to 133 us, 440 to 470 TFLOP/s.
 constexpr int kTileRows = 128;
 
 using float16v = float __attribute__((ext_vector_type(16)));
