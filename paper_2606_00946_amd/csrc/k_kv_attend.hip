@@ -116,9 +116,13 @@ constexpr int kSplitPerCu = D == 64 ? 4 : D == 128 ? 2 : 1;
 // sequences 51.0 and 53.5; 8: 16.9 and 50.9.
 constexpr int kMinUnits = 8;
 constexpr float kNoMax = -3e38f;     // reference of nothing: below every logit
-// log2 of a row's largest weight when the reference moves up to it: all of a lane's tokens of
-// a step (8 and 32) may have it within kMostWeight, and later ones twice and eight times that.
+// A logit's weight is 2^(logit - reference).  log2 of a row's largest weight when the
+// reference moves up: all of a lane's tokens of a step (8 and 32) may have it within
+// kMostWeight, and later ones twice and eight times that.
 constexpr float kSplitTop = 12.0f, kTileTop = 8.0f;
+// The reference under which a largest logit mx has that weight; from 2^26 on, where the
+// difference could be rounded to 16, the weight 1.
+__device__ __forceinline__ float raised(float m, float mx, float top) { return fmaxf(m, fabsf(mx) < 0x1p+26f ? mx - top : mx); }
 // Bounds of the sum of a lane's weights in a step (8 or 32 tokens), beyond which the reference
 // may move.  No weight is too large for a half; and an error of 2^-25, where a weight has less
 // than 11 bits, is 2^-16 of the sum.  Steps that the mask cuts have lanes with one token or
@@ -130,15 +134,14 @@ constexpr float kLeast = -9.0f, kLeastCut = -14.0f;       // log2
 __device__ __forceinline__ bool off_range(float sum, bool cut) {
     return (sum > kMostWeight) | ((sum < (cut ? 0x1p-14f : 0x1p-9f)) & (sum > 0.0f));
 }
-// Whether all weights of a row in the step are below that, mx being its largest logit and
-// 2^top the weight that the reference m stands for.
-__device__ __forceinline__ bool is_low(float m, float mx, float top, bool cut) {
-    return (mx - m < (cut ? kLeastCut : kLeast) - top) & (mx > -INFINITY);
+// Whether all weights of a row in the step are below that, mx being its largest logit and m the reference.
+__device__ __forceinline__ bool is_low(float m, float mx, bool cut) {
+    return (mx - m < (cut ? kLeastCut : kLeast)) & (mx > -INFINITY);
 }
 // The reference that makes the largest 1, as far as the sums have room, `most` being their largest magnitude.
-__device__ __forceinline__ float lowered(float m, float mx, float top, float most) {
+__device__ __forceinline__ float lowered(float m, float mx, float most) {
     const float room = fmaxf(100.0f - __builtin_amdgcn_logf(fmaxf(most, 1.0f)), 0.0f);
-    return fmaxf(mx + top, m - room);
+    return fmaxf(mx, m - room);
 }
 
 // A sequence of the call as split_part sees it; units of one kv head, 0: too many rows for it.
@@ -479,7 +482,7 @@ __device__ __forceinline__ void split_part(const KvView& c, const AttnArgs& a, b
                     float w[4];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        w[k] = __builtin_amdgcn_exp2f(x[e][k] - (m_run - kSplitTop));
+                        w[k] = __builtin_amdgcn_exp2f(x[e][k] - m_run);
                         p[4 * e + k] = (_Float16)w[k];
                     }
                     sum[e] = (w[0] + w[1]) + (w[2] + w[3]);
@@ -494,8 +497,8 @@ __device__ __forceinline__ void split_part(const KvView& c, const AttnArgs& a, b
                     for (int k = 0; k < 4; ++k) mx = fmaxf(mx, x[e][k]);
                 mx = fmaxf(mx, __shfl_xor(mx, 16));
                 mx = fmaxf(mx, __shfl_xor(mx, 32));
-                float to = fmaxf(m_run, mx);
-                const bool low = is_low(m_run, mx, kSplitTop, masked);
+                float to = raised(m_run, mx, kSplitTop);
+                const bool low = is_low(m_run, mx, masked);
                 if (__any(low)) {
                     float most = l_run;
 #pragma unroll
@@ -506,7 +509,7 @@ __device__ __forceinline__ void split_part(const KvView& c, const AttnArgs& a, b
                             for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(o[dt][k][i]));
                     most = fmaxf(most, __shfl_xor(most, 16));
                     most = fmaxf(most, __shfl_xor(most, 32));
-                    to = low ? lowered(m_run, mx, kSplitTop, most) : to;
+                    to = low ? lowered(m_run, mx, most) : to;
                 }
                 const float by = __builtin_amdgcn_exp2f(m_run - to);
                 m_run = to;
@@ -842,12 +845,12 @@ __device__ __forceinline__ void tile_part(const KvView& c, const AttnArgs& a, in
         auto weigh = [&](auto rounded) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float log = of_lane(log_scale, 4 + e), ref = m_run - kTileTop, off = log - ref;
+                const float log = of_lane(log_scale, 4 + e), off = log - m_run;
                 sum[e] = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float x = s[e >> 1][(e & 1) * 8 + i];
-                    const float w = __builtin_amdgcn_exp2f(rounded ? fmaf(x, f[e], log) - ref : fmaf(x, f[e], off));
+                    const float w = __builtin_amdgcn_exp2f(rounded ? fmaf(x, f[e], log) - m_run : fmaf(x, f[e], off));
                     sum[e] += w;
                     p[e][i] = (_Float16)w;
                 }
@@ -867,8 +870,8 @@ __device__ __forceinline__ void tile_part(const KvView& c, const AttnArgs& a, in
                 mx = fmaxf(mx, fmaf(top, f[e], of_lane(log_scale, 4 + e)));
             }
             mx = fmaxf(mx, __shfl_xor(mx, 32));
-            float to = fmaxf(m_run, mx);
-            const bool low = is_low(m_run, mx, kTileTop, masked);
+            float to = raised(m_run, mx, kTileTop);
+            const bool low = is_low(m_run, mx, masked);
             if (__any(low)) {
                 float most = l_run;
 #pragma unroll
@@ -876,7 +879,7 @@ __device__ __forceinline__ void tile_part(const KvView& c, const AttnArgs& a, in
 #pragma unroll
                     for (int k = 0; k < 16; ++k) most = fmaxf(most, fabsf(o[i][k]));
                 most = fmaxf(most, __shfl_xor(most, 32));
-                to = low ? lowered(m_run, mx, kTileTop, most) : to;
+                to = low ? lowered(m_run, mx, most) : to;
             }
             if (__any((to != m_run) | (level > kMostWeight))) {
                 const float by = __builtin_amdgcn_exp2f(m_run - to);

@@ -134,7 +134,7 @@ def first_token_takes(ctx, H, G, D, past, new, lift, rest, fmt, kind, window=0, 
     scale, N = D ** -0.5, window or past + new // 2
     # values of one sign and large enough for the output's format
     k, v = (t.view(torch.uint8) for t in s.bufs[:2])
-    v.copy_(torch.randint(0x40, 0x70, v.shape, device="cuda", dtype=torch.uint8))
+    v.copy_(torch.from_numpy(s.rng.randint(0x40, 0x70, tuple(v.shape)).astype(np.uint8)))
     s.bufs[3].fill_(4.0 if fmt == "fp8" else 8.0)
     s.bufs[3].view(s.n_pages, H)[int(s.table[0, 0])] *= lift
     s.bufs[2].fill_(2.0 ** -8 if fmt == "fp8" else 2.0 ** -6)
@@ -187,7 +187,7 @@ def test_huge_logits(ctx, G, seqs, kind, log_q, log_scale, sign, window):  # noq
     import torch
     s = Setup(seqs, kind=kind, seed=51)
     k = s.bufs[0].view(torch.uint8)
-    k.copy_(torch.randint(0x40, 0x70, k.shape, device="cuda", dtype=torch.uint8))
+    k.copy_(torch.from_numpy(s.rng.randint(0x40, 0x70, tuple(k.shape)).astype(np.uint8)))
     s.bufs[2].fill_(2.0 ** (50 if log_q == 50 else 64 if log_q == 15 else 8))
     q = torch.full((s.T, s.H * G, s.D), sign * 2.0 ** log_q, dtype=s.kind, device="cuda")
     s.tensor = lambda *a: q
@@ -211,3 +211,36 @@ def test_nan_and_infinite_queries(ctx, G, seqs):  # noqa: F811
     ctx.ls_kv_attention(s.cache, s.batch, q, out)
     torch.cuda.synchronize()
     assert torch.equal(out[~bad], clean[~bad])
+
+
+@pytest.mark.parametrize("sign", [-1, 1])
+@pytest.mark.parametrize("exponent", list(range(16, 36)))
+def test_large_logits_of_every_size(ctx, exponent, sign):  # noqa: F811
+    """Logits around 2^exponent, where the last bit of one is worth 2^-9 to 2^11: rows that see one token, one page that
+    takes all, and equal keys."""
+    import torch
+    s = Setup([(0, 1), (200, 1), (0, 150), (33, 90)], H=1, kind="f16", seed=exponent)
+    codes = s.rng.randint(0x40, 0x70, (s.n_pages, s.D)).astype(np.uint8)
+    k, at = s.bufs[0].view(torch.uint8).view(s.n_pages, -1), ko.offsets(s.page, s.D, False)
+    rows = np.zeros((s.n_pages, s.page * s.D), np.uint8)
+    rows[:, at] = codes[:, None]
+    k.copy_(torch.from_numpy(rows))
+    s.bufs[2].fill_(1.0)
+    q = torch.full((s.T, 4, s.D), sign * 2.0 ** (exponent - 24), dtype=s.kind, device="cuda")
+    s.tensor = lambda *a: q
+    for window in (1, 16):
+        note(f"kv large logits 2^{exponent} {sign} window={window}")
+        check_attention(ctx, s, 4, window=window, scale=1024.0)
+    # every page's keys alike: tokens weigh alike, as far as fp32 logits of this size tell.  The product and its sum with
+    # the value scale's logarithm are each rounded to 2^-24 of the logit, which is below 2^(exponent - 1.5).
+    k.copy_(k[:1].expand_as(k).clone())
+    note(f"kv large logits 2^{exponent} {sign} equal")
+    out = torch.empty_like(q)
+    ctx.ls_kv_attention(s.cache, s.batch, q, out, scale=1024.0)
+    want, mag = ko.attention(s.host(), q.double().cpu().numpy(), s.off, s.past, s.table, 1024.0)
+    off = np.abs(out.double().cpu().numpy() - want)
+    weights = np.expm1(np.log(2.0) * 2.0 ** (exponent - 24.5)) if exponent < 25 else 0.0
+    if weights:
+        assert (off <= 2.0 ** -10 * np.abs(want) + (2.0 ** -9 + weights) * mag + 1e-7).all()
+    top = max(float(np.abs(s.host().tokens("v", s.table[b], int(s.past[b] + s.new[b]))[0]).max()) for b in range(4))
+    assert float(out.abs().max()) <= top * (1 + 2.0 ** -9)
