@@ -602,6 +602,93 @@ int ls_kv_attention(ls_ctx* ctx, const ls_kv_cache* cache, const ls_kv_batch* ba
 int ls_kv_read(ls_ctx* ctx, const ls_kv_cache* cache, const ls_kv_batch* batch, void* k_out, void* v_out, void* stream);
 
 /*
+ * Drafts and pages of the KV cache.  An instance that drafts tokens appends a tree
+ * of them behind a sequence's cached ones (token past + j of the sequence being
+ * new token j, whatever its depth), lets every draft attend over the cache and its
+ * own ancestors, and keeps one path.  ls_kv_append_at and ls_kv_attention_tree
+ * work on one layer's cache like the calls above, the others on all layers'
+ * caches in one call: `caches` is a host array of n_caches of them, all with the
+ * same dtype, n_kv_heads, head_dim, page_tokens and n_pages.
+ *
+ * ls_positions  positions of the call's rows for the rotation (host struct):
+ *   n_axes       1..LS_MAX_AXES
+ *   pos          DEVICE int32 [n_axes x n_tokens]: row t stands at pos[a * n_tokens + t] on axis a (time, height
+ *                and width of an image's patches, a draft's depth); below 0 counts as 0, n_positions and beyond
+ *                as the last table row
+ *   axis         HOST uint8 [rotary / 2]: rotary pair i turns by column i of the table at its axis' position
+ *                (NULL: all by axis 0); copied before return
+ * ls_tree  what the call's rows see of their sequence's new tokens (host struct of device arrays):
+ *   mask         uint64 [n_tokens x mask_words], 64 * mask_words >= max_new: bit j % 64 of word j / 64 of a row says
+ *                that it sees new token j of its sequence (bits from the sequence's new tokens on do not count)
+ *   pos          int32 [n_tokens]: the rows' positions, for the window only (NULL without one); below past[b]
+ *                counts as past[b]
+ *
+ * ls_kv_append_at  ls_kv_append with the keys and queries turned by `positions`; rows are stored where
+ *   ls_kv_append stores them.  rope and positions must be given.
+ * ls_kv_attention_tree  ls_kv_attention with another choice of visible tokens: a cached token j < past is
+ *   visible to a row at position p when window is 0, j > p - window or j < sinks; new token j when the row's
+ *   mask has its bit (itself included).  A row that sees nothing gets 0.  What a token that no row sees holds
+ *   does not reach any result.  Numerics and workspace are those of ls_kv_attention, with one
+ *   difference: rows are 32 or 64 to a tile, whatever their number.
+ * ls_kv_keep  keeps a path of each sequence's drafts: new token kept[new_off[b] + i] of sequence b becomes
+ *   new token i, for i < n_kept[b] (kept int32 [n_tokens], n_kept int32 [n_seqs], both on the device), in
+ *   all layers; past[b] grows by n_kept[b] afterwards (the caller's).  A list ascends; it ends before the first
+ *   entry that does not, or is no new token of the sequence.  A token whose old or new page is absent
+ *   stays where it is.  A page that tokens move into gets the larger of its scale and the one that the largest
+ *   magnitude among them asks for (ls_kv_append's rule), and what it holds up to the last kept token is brought
+ *   to it; codes are rounded once more where the scales differ.  What lies behind the last kept token is nobody's.
+ * ls_kv_fork  for i < n_forks, row dst[i] of pages_out takes over the first tokens[i] tokens of row src[i] of
+ *   pages (tables int32 [n_rows x pages_stride]; src, dst, tokens int32 [n_forks], all on the device): entries of
+ *   pages that these tokens fill are copied, so both rows share them; where the last page is only partly filled, its
+ *   16-token blocks that hold some of them, and its scales, are copied in all layers onto the page that
+ *   pages_out[dst[i]] has in that place (the caller's fresh page; if it is the same page, or either is
+ *   absent, nothing is copied).  Other entries stay.  A fork with a row outside the table is left out; tokens
+ *   is taken into [0, pages_stride * page_tokens].  pages_out may be pages if no row is both a
+ *   source and a destination.  No row may be the destination twice, and no page that is copied onto may be
+ *   copied from or onto by another fork: its contents would be either's.
+ * ls_kv_compact  moves the pages in use to the lowest ids, in all layers: of the U distinct ids that `pages`
+ *   names (those outside [0, n_pages) are absent), the k-th lowest from U on goes to the k-th lowest id below U
+ *   that is not named; the others stay.  pages_out (may be pages) gets the table with the new ids, absent entries as they
+ *   are; where int32 [n_pages] every page's new id, -1 for those not named; n_used int32 [1] gets U: pages from
+ *   there on are free.  A page kept for later requests must be named too (in a row of its own, say).  For pools
+ *   of up to 16 million pages (beyond: LS_ERR_UNSUPPORTED).
+ *
+ * All are asynchronous on `stream`, need neither model nor cache state, validate on
+ * the host, and read and write device arrays only in bounds whatever these hold.
+ * ls_kv_attention_tree and ls_kv_compact use ls_kv_attention's workspace, with its
+ * rules: calls of the three on several streams of one context are ordered by the
+ * caller, and so are replays of graphs that hold them; one of them is made before
+ * the first is captured.
+ */
+#define LS_MAX_AXES 4
+
+typedef struct {
+    int32_t n_axes;
+    const int32_t* pos;
+    const uint8_t* axis;
+} ls_positions;
+
+typedef struct {
+    const uint64_t* mask;
+    int32_t mask_words;
+    const int32_t* pos;
+} ls_tree;
+
+int ls_kv_append_at(ls_ctx* ctx, const ls_kv_cache* cache, const ls_kv_batch* batch, const ls_rope* rope,
+                    const ls_positions* positions, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                    const void* q, int64_t q_stride, int32_t n_q_heads, void* q_out, int64_t q_out_stride, void* stream);
+int ls_kv_attention_tree(ls_ctx* ctx, const ls_kv_cache* cache, const ls_kv_batch* batch, const ls_tree* tree,
+                         const void* q, int64_t q_stride, int32_t n_q_heads, float scale, int32_t window, int32_t sinks,
+                         void* out, int64_t out_stride, void* stream);
+int ls_kv_keep(ls_ctx* ctx, const ls_kv_cache* caches, int32_t n_caches, const ls_kv_batch* batch, const int32_t* kept,
+               const int32_t* n_kept, void* stream);
+int ls_kv_fork(ls_ctx* ctx, const ls_kv_cache* caches, int32_t n_caches, int32_t n_rows, int32_t pages_stride,
+               const int32_t* pages, int32_t* pages_out, int32_t n_forks, const int32_t* src, const int32_t* dst,
+               const int32_t* tokens, void* stream);
+int ls_kv_compact(ls_ctx* ctx, const ls_kv_cache* caches, int32_t n_caches, int32_t n_rows, int32_t pages_stride,
+                  const int32_t* pages, int32_t* pages_out, int32_t* where, int32_t* n_used, void* stream);
+
+/*
  * Per-kernel timing (the library's own view of where the routing time goes;
  * Section 5.4 measures the router's overhead end to end).  While enabled, each
  * kernel launch group of the context is bracketed by HIP events on the stream
@@ -609,7 +696,7 @@ int ls_kv_read(ls_ctx* ctx, const ls_kv_cache* cache, const ls_kv_batch* batch, 
  * cost no cache writeback).  Kinds: "table_build", "prefix_match", "instance_partial",
  * "score_pairs", "score_pairs_mfma", "band_select", "rescore", "argmin",
  * "update", "route", "buffer", "index" (prefix-index maintenance), "kv_append",
- * "kv_attention", "kv_read".
+ * "kv_attention", "kv_read", "kv_tree", "kv_keep", "kv_fork", "kv_compact".
  *   ls_profile_enable  enable != 0 starts recording (and clears old records).
  *   ls_profile_read    synchronous; for up to max_kinds kinds writes the kind
  *                      name (static string), the number of launches and the

@@ -7,6 +7,7 @@
 #include <algorithm>
 
 #include "k_kv.h"
+#include "ls_kv_calls.h"
 
 namespace ls {
 namespace {
@@ -48,6 +49,33 @@ __device__ __forceinline__ Turn turn_of(const KvRope& r, const Unit& t, int u, i
         for (int i = 0; i < 2; ++i) {
             f.c[i] = reinterpret_cast<const float4v*>(r.cos + at)[i];
             f.s[i] = reinterpret_cast<const float4v*>(r.sin + at)[i];
+        }
+    }
+    return f;
+}
+
+// Where the positions of a call's rows come from: their places in their sequences,
+// an axis for each unit of pairs, or an axis for each pair.
+enum Where { PLACE, UNIT, PAIR };
+
+__device__ __forceinline__ int axis_of(const KvPositions& at, int pair) { return at.axis[pair >> 4] >> 2 * (pair & 15) & 3; }
+
+// The same of the call's row t on the axes of the unit's pairs; a position below 0 counts as 0.  A
+// unit on one axis costs one more load; one on several axes reads its pairs' angles one by one.
+template <Where AT>
+__device__ __forceinline__ Turn turn_at(const KvRope& r, const KvPositions& at, const Unit& t, int u, int64_t pos, int64_t row,
+                                        int32_t T) {
+    if constexpr (AT == PLACE) return turn_of(r, t, u, pos);
+    if constexpr (AT == UNIT)
+        return turn_of(r, t, u, t.turns ? max(at.pos[(int64_t)axis_of(at, u * 8) * T + row], 0) : 0);
+    Turn f = {{{1, 1, 1, 1}, {1, 1, 1, 1}}, {{0, 0, 0, 0}, {0, 0, 0, 0}}};
+    if (t.turns) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int32_t p = at.pos[(int64_t)axis_of(at, u * 8 + i) * T + row];
+            const int64_t e = (int64_t)min(max(p, 0), r.n_pos - 1) * (r.rotary >> 1) + u * 8 + i;
+            f.c[i >> 2][i & 3] = r.cos[e];
+            f.s[i >> 2][i & 3] = r.sin[e];
         }
     }
     return f;
@@ -101,9 +129,11 @@ __device__ __forceinline__ uint32_t regraded(uint32_t w, float again) {
 }
 
 // A page's rows [row0, row1) are new; `src` is row row0's, `pos0` the page's first
-// position, `held` the scale of the rows before row0 (0: there are none).
+// position, `row` the call's row of row0.
 struct PageWork {
-    int64_t page, pos0;
+    int64_t page, pos0, row;
+    // The call's row of the page's row i, or of the new one next to it.
+    __device__ __forceinline__ int64_t row_of(int i) const { return row + min(max(i, row0), row1 - 1) - row0; }
     const uint16_t* src;
     int64_t stride;
     int row0, row1;
@@ -137,8 +167,9 @@ __device__ __forceinline__ void regrade_rows(uint8_t* base, int row0, float agai
 
 // One new row in the page (a decode step): a row's units side by side for as many
 // heads as a wave holds, so that one pass of loads serves them all.
-template <int D, bool FP8, bool F16, bool VALUE>
-__device__ __forceinline__ void append_row(const KvView& c, const KvRope& r, const PageWork& w, int h0, int heads) {
+template <int D, bool FP8, bool F16, bool VALUE, Where AT>
+__device__ __forceinline__ void append_row(const KvView& c, const KvRope& r, const KvPositions& at, const PageWork& w, int h0,
+                                           int heads) {
     constexpr int U = D / 16;
     const int lane = threadIdx.x & 63, u = lane % U, h = h0 + lane / U;
     const bool on = lane / U < heads;
@@ -150,7 +181,7 @@ __device__ __forceinline__ void append_row(const KvView& c, const KvRope& r, con
         raw[0] = load8(w.src + h * D + t.a);
         raw[1] = load8(w.src + h * D + t.b);
     }
-    const Turn f = turn_of(r, t, u, w.pos0 + w.row0);
+    const Turn f = turn_at<AT>(r, at, t, u, w.pos0 + w.row0, w.row, c.T);
     float x[16];
     widen8<F16>(raw[0], x);
     widen8<F16>(raw[1], x + 8);
@@ -188,8 +219,8 @@ __device__ __forceinline__ void append_row(const KvView& c, const KvRope& r, con
 // tokens.  A page of one block (ONE; `turns`: its positions' table rows)
 // stays in registers between finding the scale and writing the codes; larger ones
 // are read again, from the caches.
-template <int D, bool FP8, bool F16, bool VALUE, bool ONE>
-__device__ __forceinline__ void append_page(const KvView& c, const KvRope& r, const PageWork& w, int h,
+template <int D, bool FP8, bool F16, bool VALUE, bool ONE, Where AT>
+__device__ __forceinline__ void append_page(const KvView& c, const KvRope& r, const KvPositions& at, const PageWork& w, int h,
                                             const Turn (&turns)[D / 64]) {
     constexpr int U = D / 16, N = D / 64;
     const int lane = threadIdx.x & 63;
@@ -233,7 +264,8 @@ __device__ __forceinline__ void append_page(const KvView& c, const KvRope& r, co
                 widen8<F16>(raw[n][1], x[n] + 8);
                 const int e = n * 64 + lane;
                 const Unit t = unit_of(r, e % U);
-                rotate(r, t, ONE ? turns[n] : turn_of(r, t, e % U, w.pos0 + blk * 16 + e / U), x[n]);
+                const int row = blk * 16 + e / U;
+                rotate(r, t, ONE ? turns[n] : turn_at<AT>(r, at, t, e % U, w.pos0 + row, w.row_of(row), c.T), x[n]);
             } else {
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
@@ -291,8 +323,8 @@ __device__ __forceinline__ void append_page(const KvView& c, const KvRope& r, co
 // them rotate a row of the queries each, as many heads at a time as a wave holds.
 // Measured: 69k tokens of 8 kv and 32 query heads of 128: 305 us, 5.1 TB/s; 256 single
 // tokens 6.2 us; one token 3.1 us.
-template <int D, bool FP8, bool F16>
-__global__ __launch_bounds__(256) void kv_append_kernel(KvView c, KvRope r, const uint16_t* __restrict__ k,
+template <int D, bool FP8, bool F16, Where AT>
+__global__ __launch_bounds__(256) void kv_append_kernel(KvView c, KvRope r, KvPositions at, const uint16_t* __restrict__ k,
                                                         int64_t k_stride, const uint16_t* __restrict__ v,
                                                         int64_t v_stride, const uint16_t* q, int64_t q_stride,
                                                         int32_t Hq, uint16_t* q_out, int64_t q_out_stride,
@@ -320,12 +352,13 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvView c, KvRope r, cons
         p.page = page_id(c, b, (int)its.j);
         if (p.page < 0) return;
         p.stride = value ? v_stride : k_stride;
-        p.src = (value ? v : k) + (t0 + (p.pos0 + p.row0 - past)) * p.stride;
+        p.row = t0 + (p.pos0 + p.row0 - past);
+        p.src = (value ? v : k) + p.row * p.stride;
         const int hn = min(heads, c.H - h0);
         auto append = [&](auto is_value) {
             constexpr bool V = decltype(is_value)::value;
             if (p.row1 - p.row0 == 1) {
-                append_row<D, FP8, F16, V>(c, r, p, h0, hn);
+                append_row<D, FP8, F16, V, V ? PLACE : AT>(c, r, at, p, h0, hn);
                 return;
             }
             Turn turns[D / 64] = {};
@@ -334,11 +367,11 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvView c, KvRope r, cons
 #pragma unroll
                     for (int i = 0; i < D / 64; ++i) {
                         const int e = i * 64 + lane;
-                        turns[i] = turn_of(r, unit_of(r, e % U), e % U, p.pos0 + e / U);
+                        turns[i] = turn_at<AT>(r, at, unit_of(r, e % U), e % U, p.pos0 + e / U, p.row_of(e / U), c.T);
                     }
-                for (int i = 0; i < hn; ++i) append_page<D, FP8, F16, V, true>(c, r, p, h0 + i, turns);
+                for (int i = 0; i < hn; ++i) append_page<D, FP8, F16, V, true, AT>(c, r, at, p, h0 + i, turns);
             } else {
-                for (int i = 0; i < hn; ++i) append_page<D, FP8, F16, V, false>(c, r, p, h0 + i, turns);
+                for (int i = 0; i < hn; ++i) append_page<D, FP8, F16, V, false, AT>(c, r, at, p, h0 + i, turns);
             }
         };
         if (value) append(std::true_type{}); else append(std::false_type{});
@@ -346,11 +379,14 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvView c, KvRope r, cons
     }
     const int64_t t = (int64_t)w - n_items;
     if (!q || t >= c.T) return;
-    const int b = seq_of_slot(c, t, [](int off, int) { return (int64_t)off; });
-    const int64_t pos = max((int64_t)max(c.past[b], 0) + t - min(max(c.off[b], 0), c.T), (int64_t)0);
+    int64_t pos = 0;
+    if constexpr (AT == PLACE) {
+        const int b = seq_of_slot(c, t, [](int off, int) { return (int64_t)off; });
+        pos = max((int64_t)max(c.past[b], 0) + t - min(max(c.off[b], 0), c.T), (int64_t)0);
+    }
     const int u = lane % U;
     const Unit m = unit_of(r, u);
-    const Turn f = turn_of(r, m, u, pos);
+    const Turn f = turn_at<AT>(r, at, m, u, pos, t, c.T);
     const uint16_t* src = q + t * q_stride;
     uint16_t* dst = q_out + t * q_out_stride;
     // a lane reads all that it writes first: q_out may be q
@@ -439,9 +475,9 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvView c, uint16_t* __rest
 
 }  // namespace
 
-hipError_t launch_kv_append(const KvView& c, const KvRope& r, const void* k, int64_t k_stride, const void* v,
-                            int64_t v_stride, const void* q, int64_t q_stride, int32_t Hq, void* q_out,
-                            int64_t q_out_stride, int n_cu, hipStream_t s) {
+hipError_t launch_kv_append_at(const KvView& c, const KvRope& r, const KvPositions& at, const void* k, int64_t k_stride,
+                               const void* v, int64_t v_stride, const void* q, int64_t q_stride, int32_t Hq, void* q_out,
+                               int64_t q_out_stride, int n_cu, hipStream_t s) {
     const int64_t slots = (int64_t)(c.T >> c.page_shift) + 2 * (int64_t)c.B;
     // heads a wave takes in turn: all that one pass of a single row's loads serves, fewer while that leaves waves idle
     int heads = std::min(c.H, 1024 / c.D);
@@ -451,15 +487,27 @@ hipError_t launch_kv_append(const KvView& c, const KvRope& r, const void* k, int
     if (groups >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
     return by_types(c, [&](auto fp8, auto f16) {
         auto run = [&](auto d) {
-            kv_append_kernel<decltype(d)::value, fp8.value, f16.value><<<(uint32_t)groups, 256, 0, s>>>(
-                c, r, (const uint16_t*)k, k_stride, (const uint16_t*)v, v_stride, (const uint16_t*)q, q_stride, Hq,
-                (uint16_t*)q_out, q_out_stride, (uint32_t)n_items, heads);
-            return hipGetLastError();
+            auto launch = [&](auto where) {
+                kv_append_kernel<decltype(d)::value, fp8.value, f16.value, decltype(where)::value>
+                    <<<(uint32_t)groups, 256, 0, s>>>(c, r, at, (const uint16_t*)k, k_stride, (const uint16_t*)v, v_stride,
+                                                      (const uint16_t*)q, q_stride, Hq, (uint16_t*)q_out, q_out_stride,
+                                                      (uint32_t)n_items, heads);
+                return hipGetLastError();
+            };
+            if (at.n_axes == 0) return launch(std::integral_constant<Where, PLACE>{});
+            if (at.mixed) return launch(std::integral_constant<Where, PAIR>{});
+            return launch(std::integral_constant<Where, UNIT>{});
         };
         if (c.D == 64) return run(std::integral_constant<int, 64>{});
         if (c.D == 128) return run(std::integral_constant<int, 128>{});
         return run(std::integral_constant<int, 256>{});
     });
+}
+
+hipError_t launch_kv_append(const KvView& c, const KvRope& r, const void* k, int64_t k_stride, const void* v,
+                            int64_t v_stride, const void* q, int64_t q_stride, int32_t Hq, void* q_out,
+                            int64_t q_out_stride, int n_cu, hipStream_t s) {
+    return launch_kv_append_at(c, r, KvPositions{}, k, k_stride, v, v_stride, q, q_stride, Hq, q_out, q_out_stride, n_cu, s);
 }
 
 hipError_t launch_kv_read(const KvView& c, void* k_out, void* v_out, hipStream_t s) {

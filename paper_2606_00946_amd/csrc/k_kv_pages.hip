@@ -1,0 +1,424 @@
+// What moves tokens and pages of the paged 8-bit KV cache (k_kv.h) between steps,
+// in all layers at once: keeping drafts, forking sequences, compaction.  All three
+// copy codes, so HBM bounds the large calls and the chain of dependent reads
+// (lengths, table, codes) the small ones.
+#include <algorithm>
+
+#include "k_kv.h"
+#include "ls_kv_calls.h"
+#include "ls_scratch.h"
+
+namespace ls {
+namespace {
+
+// ---- keeping drafts ---------------------------------------------------------------
+
+// A sequence's kept tokens: the list ends before the first entry that is not above
+// the one before it, or not one of the new tokens.  Kept token i comes from new
+// token kept[i] >= i, so a page's tokens come from it or from later pages, and
+// pages may be rewritten in their order.
+__device__ __forceinline__ int kept_count(const int32_t* kept, int want, int n) {
+    const int lane = threadIdx.x & 63;
+    want = min(max(want, 0), n);
+    for (int i0 = 0; i0 < want; i0 += 64) {
+        const int i = i0 + lane;
+        const int32_t k = i < want ? kept[i] : n, before = i > 0 && i < want ? kept[i - 1] : -1;
+        const uint64_t bad = __ballot(k <= before || k >= n);
+        if (bad) return min(i0 + __ffsll((long long)bad) - 1, want);
+    }
+    return want;
+}
+
+// Where a token lies: its page, or -1, and its row there.
+struct Spot {
+    int32_t page, row;
+};
+__device__ __forceinline__ Spot spot_of(const KvView& c, int b, int64_t pos) {
+    const int64_t j = pos >> c.page_shift;
+    return {j < c.W ? (int32_t)page_id(c, b, (int)j) : -1, (int32_t)pos & (c.page - 1)};
+}
+
+// Largest magnitude of four codes.
+template <bool FP8>
+__device__ __forceinline__ float top_of(uint32_t w) {
+    const float4v f = code_values<FP8>(w);
+    return fmaxf(fmaxf(fabsf(f.x), fabsf(f.y)), fmaxf(fabsf(f.z), fabsf(f.w)));
+}
+
+template <bool FP8>
+__device__ __forceinline__ uint32_t regraded(uint32_t w, float again) {
+    const float4v f = code_values<FP8>(w);
+    return codes_of<FP8>(f.x * again, f.y * again, f.z * again, f.w * again);
+}
+
+// A wave: one layer's keys or values of a sequence and head.  Page by page, 16 tokens
+// at a time: a lane holds, of every 64 dimensions, 16 of one key, or four of each of four
+// values.  Once for the largest magnitude that moves in, once for the codes; a page of
+// 16 tokens stays in registers between the two.
+template <int D, bool FP8, bool VALUE>
+__device__ __forceinline__ void keep_rows(const KvView& c, uint8_t* codes, float* scales, int b, int h, int64_t past,
+                                          const int32_t* kept, int n) {
+    constexpr int ND = D / 64, NT = VALUE ? 4 : 1;       // tokens of a lane
+    const int lane = threadIdx.x & 63;
+    const int first = VALUE ? (lane >> 4) * 4 : lane >> 2;      // the lane's first token of a block
+    const int64_t head = (int64_t)c.page * D;
+    for (int64_t j = past >> c.page_shift; j << c.page_shift < past + n; ++j) {
+        const int64_t pos0 = j << c.page_shift;
+        const int r0 = (int)max(past - pos0, (int64_t)0), r1 = (int)min(past + n - pos0, (int64_t)c.page);
+        const int64_t page = j < c.W ? page_id(c, b, (int)j) : -1;
+        if (page < 0) continue;
+        uint8_t* mine = codes + (page * c.H + h) * head;
+        const float held = scales[page * c.H + h];
+        uint4v x[NT][ND];
+        float from[NT];                  // the tokens' scales
+        bool moves[NT];
+        auto load = [&](int blk) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const int row = blk * 16 + first + t;
+                Spot s = {(int32_t)page, row};
+                if (row >= r0 && row < r1) {
+                    const int i = (int)(pos0 + row - past);
+                    const int32_t k = kept[i];
+                    if (k != i) s = spot_of(c, b, past + k);
+                }
+                moves[t] = s.page >= 0 && (s.page != page || s.row != row);
+                if (s.page < 0) s = {(int32_t)page, row};
+                const int64_t at = (int64_t)s.page * c.H + h;
+                from[t] = scales[at];
+                const uint8_t* p = codes + at * head + (s.row >> 4) * 16 * D;
+                const int byte = VALUE ? ((s.row & 15) >> 2) * 256 + (lane & 15) * 16 : (s.row & 15) * 64 + (lane & 3) * 16;
+#pragma unroll
+                for (int d = 0; d < ND; ++d) {
+                    x[t][d] = *reinterpret_cast<const uint4v*>(p + d * 1024 + byte);
+                    if constexpr (VALUE)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[t][d][e] = x[t][d][e] >> 8 * (s.row & 3) & 255u;
+                }
+            }
+        };
+        float top = 0.0f;
+        uint64_t any = 0;
+        const int b0 = r0 >> 4, b1 = (r1 + 15) >> 4;
+        for (int blk = b0; blk < b1; ++blk) {
+            load(blk);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                any |= __ballot(moves[t]);
+                float m = 0.0f;
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) m = fmaxf(m, top_of<FP8>(x[t][d][e]));
+                top = fmaxf(top, moves[t] ? m * from[t] : 0.0f);
+            }
+        }
+        if (!any) continue;
+        const float scale = fmaxf(scale_of<FP8>(wave_max(top)), held), inv = 1.0f / scale;
+        int loaded = b1 - 1;
+        for (int blk = scale > held ? 0 : b0; blk < b1; ++blk) {
+            if (blk != loaded) load(blk);
+            loaded = blk;
+            uint8_t* p = mine + blk * 16 * D;
+            // the block's tokens may come from later rows of it: all have been read before any lane writes
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            if constexpr (!VALUE) {
+                if (blk * 16 + first < r1 && (moves[0] || scale > held)) {
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) {
+                        uint4v o;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[e] = regraded<FP8>(x[0][d][e], from[0] * inv);
+                        *reinterpret_cast<uint4v*>(p + d * 1024 + first * 64 + (lane & 3) * 16) = o;
+                    }
+                }
+            } else {
+                const int live = r1 - (blk * 16 + first);        // of the lane's four tokens; the others' bytes stay
+                if (live > 0) {
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) {
+                        uint4v* at = reinterpret_cast<uint4v*>(p + d * 1024) + lane;
+                        const uint4v old = live < 4 ? *at : uint4v{0, 0, 0, 0};
+                        uint4v o;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            uint32_t w = 0;
+#pragma unroll
+                            for (int t = 0; t < 4; ++t)
+                                w |= (regraded<FP8>(x[t][d][e], from[t] * inv) & 255u) << 8 * t;
+                            const uint32_t m = live < 4 ? (1u << 8 * live) - 1 : ~0u;
+                            o[e] = (w & m) | (old[e] & ~m);
+                        }
+                        *at = o;
+                    }
+                }
+            }
+        }
+        if (lane == 0 && scale > held) scales[page * c.H + h] = scale;
+    }
+}
+
+// Waves: (layer, sequence, head, key or value).
+template <int D, bool FP8>
+__global__ __launch_bounds__(256) void kv_keep_kernel(KvView c, KvLayers l, const int32_t* __restrict__ kept,
+                                                      const int32_t* __restrict__ n_kept, uint32_t n_items) {
+    const uint32_t w = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    if (w >= n_items) return;
+    const int value = w & 1, h = (int)((w >> 1) % (uint32_t)c.H);
+    const uint32_t rest = (w >> 1) / (uint32_t)c.H;
+    const int b = (int)(rest % (uint32_t)c.B), layer = (int)(rest / (uint32_t)c.B);
+    int t0, n;
+    seq_rows(c, b, t0, n);
+    const int64_t past = min(max(c.past[b], 0), 1 << 30);
+    n = kept_count(kept + t0, n_kept[b], n);
+    if (n == 0) return;
+    if (value)
+        keep_rows<D, FP8, true>(c, l.codes[1][layer], l.scales[1][layer], b, h, past, kept + t0, n);
+    else
+        keep_rows<D, FP8, false>(c, l.codes[0][layer], l.scales[0][layer], b, h, past, kept + t0, n);
+}
+
+// ---- forking ----------------------------------------------------------------------
+
+// The first workgroups write the tables, 256 entries of a fork each; a wave of the
+// others copies, for a fork and layer, one head's keys or values of the last page.
+__global__ __launch_bounds__(256) void kv_fork_kernel(KvView c, KvLayers l, KvForks f, uint32_t table_groups,
+                                                      uint32_t n_items) {
+    auto known = [&](int i, int& s, int& d, int& n) {
+        s = f.src[i];
+        d = f.dst[i];
+        n = (int)min((int64_t)max(f.tokens[i], 0), (int64_t)f.W << c.page_shift);
+        return s >= 0 && s < f.rows && d >= 0 && d < f.rows;
+    };
+    int s, d, n;
+    if (blockIdx.x < table_groups) {
+        const int chunks = (f.W + 255) / 256;
+        const int i = (int)(blockIdx.x / (uint32_t)chunks), j = (int)(blockIdx.x % (uint32_t)chunks) * 256 + threadIdx.x;
+        if (known(i, s, d, n) && j < n >> c.page_shift) f.pages_out[(int64_t)d * f.W + j] = f.pages[(int64_t)s * f.W + j];
+        return;
+    }
+    const uint32_t w = __builtin_amdgcn_readfirstlane((blockIdx.x - table_groups) * 4 + (threadIdx.x >> 6));
+    if (w >= n_items) return;
+    const int lane = threadIdx.x & 63, value = w & 1, h = (int)((w >> 1) % (uint32_t)c.H);
+    const uint32_t rest = (w >> 1) / (uint32_t)c.H;
+    const int layer = (int)(rest % (uint32_t)l.n), i = (int)(rest / (uint32_t)l.n);
+    if (!known(i, s, d, n)) return;
+    const int part = n & (c.page - 1), j = n >> c.page_shift;
+    if (part == 0) return;
+    const int32_t from = f.pages[(int64_t)s * f.W + j], to = f.pages_out[(int64_t)d * f.W + j];
+    if (from < 0 || from >= c.n_pages || to < 0 || to >= c.n_pages || from == to) return;
+    const int64_t head = (int64_t)c.page * c.D, a = (int64_t)from * c.H + h, z = (int64_t)to * c.H + h;
+    const uint4v* src = reinterpret_cast<const uint4v*>(l.codes[value][layer] + a * head);
+    uint4v* dst = reinterpret_cast<uint4v*>(l.codes[value][layer] + z * head);
+    const int pieces = ((part + 15) >> 4) * c.D;             // of 16 bytes
+    constexpr int kAtOnce = 8;
+    for (int p0 = lane; p0 < pieces; p0 += 64 * kAtOnce) {
+        uint4v x[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+            if (p0 + k * 64 < pieces) x[k] = src[p0 + k * 64];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+            if (p0 + k * 64 < pieces) dst[p0 + k * 64] = x[k];
+    }
+    if (lane == 0) l.scales[value][layer][z] = l.scales[value][layer][a];
+}
+
+// ---- compaction ---------------------------------------------------------------------
+// U pages are in use.  The k-th of those from U on goes to the k-th id below U that is
+// not: as few moves as there can be, no page is read that another is written over, and
+// the same answer every time.  where[] says first which pages are in use, then which
+// move it is (-2 - k), then the page's new id.
+
+constexpr int kChunk = 4096;         // pages of a workgroup
+
+__global__ __launch_bounds__(256) void compact_clear_kernel(int32_t* where, int32_t n) {
+    const int64_t i = (int64_t)blockIdx.x * 1024 + threadIdx.x;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (i + k * 256 < n) where[i + k * 256] = -1;
+}
+
+__global__ __launch_bounds__(256) void compact_mark_kernel(KvCompact m) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < m.entries; i += (int64_t)gridDim.x * 256) {
+        const int32_t p = m.pages[i];
+        if (p >= 0 && p < m.n_pages) m.where[p] = 0;
+    }
+}
+
+// Sum over a workgroup of 256 threads, for all of them.
+__device__ __forceinline__ int32_t group_sum(int32_t x, int32_t (&lds)[4]) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+    __syncthreads();
+    return lds[0] + lds[1] + lds[2] + lds[3];
+}
+
+// Pages in use of [chunk * kChunk + from, + to).
+__device__ __forceinline__ int32_t in_use(const KvCompact& m, int64_t lo, int64_t hi) {
+    int32_t x = 0;
+    for (int64_t i = lo + threadIdx.x; i < hi; i += 256) x += m.where[i] != -1;
+    return x;
+}
+
+__global__ __launch_bounds__(256) void compact_count_kernel(KvCompact m) {
+    __shared__ int32_t lds[4];
+    const int64_t lo = (int64_t)blockIdx.x * kChunk, hi = min(lo + kChunk, (int64_t)m.n_pages);
+    const int32_t x = group_sum(in_use(m, lo, hi), lds);
+    if (threadIdx.x == 0) m.counts[blockIdx.x] = x;
+}
+
+// A chunk's pages: their places among those in use, from the chunks' counts.
+__global__ __launch_bounds__(256) void compact_emit_kernel(KvCompact m, int32_t chunks) {
+    __shared__ int32_t lds[4], wave_base[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, chunk = blockIdx.x;
+    int32_t before = 0, all = 0;
+    for (int i = threadIdx.x; i < chunks; i += 256) {
+        const int32_t x = m.counts[i];
+        all += x;
+        before += i < chunk ? x : 0;
+    }
+    before = group_sum(before, lds);
+    const int32_t used = group_sum(all, lds);
+    // places below `used` that are in use: whole chunks, and the part of the one it lies in.  That one is read while its own
+    // workgroup rewrites it: in use is whatever is not -1, before and after
+    const int32_t last = used / kChunk;
+    int32_t below = 0;
+    for (int i = threadIdx.x; i < last; i += 256) below += m.counts[i];
+    below = group_sum(below + in_use(m, (int64_t)last * kChunk, used), lds);
+    if (chunk == 0 && threadIdx.x == 0) {
+        *m.n_used = used;
+        m.counts[chunks] = used - below;             // moves
+    }
+    // a wave's quarter of the chunk, 64 pages at a time
+    const int64_t lo = (int64_t)chunk * kChunk + wave * (kChunk / 4);
+    int32_t mine = 0;
+#pragma unroll 4
+    for (int k = 0; k < kChunk / 256; ++k) {
+        const int64_t i = lo + k * 64 + lane;
+        mine += __popcll(__ballot(i < m.n_pages && m.where[i] != -1));
+    }
+    if (lane == 0) wave_base[wave] = mine;
+    __syncthreads();
+    int32_t rank = before;
+    for (int w = 0; w < wave; ++w) rank += wave_base[w];
+    for (int k = 0; k < kChunk / 256; ++k) {
+        const int64_t i = lo + k * 64 + lane;
+        const bool is = i < m.n_pages && m.where[i] != -1;
+        const uint64_t mask = __ballot(is);
+        const int32_t r = rank + __popcll(mask & ((1ull << lane) - 1));
+        rank += __popcll(mask);
+        if (i >= m.n_pages) continue;
+        if (i < used) {
+            if (is) m.where[i] = (int32_t)i; else m.to[i - r] = (int32_t)i;
+        } else if (is) {
+            m.where[i] = -2 - (r - below);
+            m.from[r - below] = (int32_t)i;
+        }
+    }
+}
+
+// The first workgroups write the table and the moved pages' new ids, the others take
+// moves in turn, a workgroup a head's keys or values in one layer at a time.
+__global__ __launch_bounds__(256) void compact_move_kernel(KvView c, KvLayers l, KvCompact m, uint32_t table_groups,
+                                                           const int32_t* n_moves) {
+    if (blockIdx.x < table_groups) {
+        const int64_t step = (int64_t)table_groups * 256;
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < m.entries; i += step) {
+            int32_t p = m.pages[i];
+            if (p >= 0 && p < m.n_pages) {
+                // a moved page's entry may be the move or, already, where it goes
+                const int32_t w = __hip_atomic_load(&m.where[p], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                p = w <= -2 ? m.to[-2 - w] : w;
+            }
+            m.pages_out[i] = p;
+        }
+        const int32_t moves = *n_moves;
+        for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < moves; k += step)
+            __hip_atomic_store(&m.where[m.from[k]], m.to[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        return;
+    }
+    const int64_t page = (int64_t)c.H * c.page * c.D / 16;       // pieces of 16 bytes
+    constexpr int kAtOnce = 4, kPiece = 256 * kAtOnce;
+    const int64_t per_page = (page + kPiece - 1) / kPiece;
+    const int64_t items = (int64_t)*n_moves * l.n * 2 * per_page;
+    for (int64_t w = blockIdx.x - table_groups; w < items; w += gridDim.x - table_groups) {
+        const int64_t piece = w % per_page, rest = w / per_page;
+        const int value = (int)(rest & 1), layer = (int)((rest >> 1) % l.n);
+        const int64_t k = (rest >> 1) / l.n;
+        const int64_t a = m.from[k], z = m.to[k];
+        const uint4v* src = reinterpret_cast<const uint4v*>(l.codes[value][layer]) + a * page;
+        uint4v* dst = reinterpret_cast<uint4v*>(l.codes[value][layer]) + z * page;
+        uint4v x[kAtOnce];
+        const int64_t p0 = piece * kPiece + threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+            if (p0 + i * 256 < page) x[i] = src[p0 + i * 256];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+            if (p0 + i * 256 < page) dst[p0 + i * 256] = x[i];
+        if (piece == 0)
+            for (int h = threadIdx.x; h < c.H; h += 256)
+                l.scales[value][layer][z * c.H + h] = l.scales[value][layer][a * c.H + h];
+    }
+}
+
+int32_t chunks_of(int64_t n_pages) { return (int32_t)((n_pages + kChunk - 1) / kChunk); }
+
+}  // namespace
+
+hipError_t launch_kv_keep(const KvView& c, const KvLayers& l, const int32_t* kept, const int32_t* n_kept, hipStream_t s) {
+    const int64_t items = (int64_t)l.n * c.B * c.H * 2, groups = (items + 3) / 4;
+    if (groups >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
+    auto run = [&](auto d, auto fp8) {
+        kv_keep_kernel<decltype(d)::value, decltype(fp8)::value>
+            <<<(uint32_t)groups, 256, 0, s>>>(c, l, kept, n_kept, (uint32_t)items);
+        return hipGetLastError();
+    };
+    auto by_dim = [&](auto fp8) {
+        if (c.D == 64) return run(std::integral_constant<int, 64>{}, fp8);
+        if (c.D == 128) return run(std::integral_constant<int, 128>{}, fp8);
+        return run(std::integral_constant<int, 256>{}, fp8);
+    };
+    return c.fp8 ? by_dim(std::true_type{}) : by_dim(std::false_type{});
+}
+
+hipError_t launch_kv_fork(const KvView& c, const KvLayers& l, const KvForks& f, bool tables, hipStream_t s) {
+    const int64_t table_groups = tables ? (int64_t)f.n * ((f.W + 255) / 256) : 0;
+    const int64_t items = (int64_t)f.n * l.n * c.H * 2, groups = table_groups + (items + 3) / 4;
+    if (groups >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
+    kv_fork_kernel<<<(uint32_t)groups, 256, 0, s>>>(c, l, f, (uint32_t)table_groups, (uint32_t)items);
+    return hipGetLastError();
+}
+
+int64_t kv_compact_bytes(int64_t n_pages) { return 4 * ((int64_t)chunks_of(n_pages) + 1 + (n_pages / 2 + 1) * 2) + 3 * 256; }
+
+// No more pages move than there are in use, nor than there are ids below.
+void kv_compact_carve(KvCompact& k, void* workspace) {
+    WsCarve ws{(char*)workspace, (size_t)kv_compact_bytes(k.n_pages)};
+    k.counts = ws.take<int32_t>(chunks_of(k.n_pages) + 1);
+    k.from = ws.take<int32_t>(k.n_pages / 2 + 1);
+    k.to = ws.take<int32_t>(k.n_pages / 2 + 1);
+}
+
+hipError_t launch_kv_compact_plan(const KvCompact& k, int n_cu, hipStream_t s) {
+    const int32_t chunks = chunks_of(k.n_pages);
+    const int64_t marks = std::min<int64_t>((k.entries + 255) / 256, (int64_t)n_cu * 8);
+    compact_clear_kernel<<<(uint32_t)(((int64_t)k.n_pages + 1023) / 1024), 256, 0, s>>>(k.where, k.n_pages);
+    if (marks > 0) compact_mark_kernel<<<(uint32_t)marks, 256, 0, s>>>(k);
+    compact_count_kernel<<<(uint32_t)chunks, 256, 0, s>>>(k);
+    compact_emit_kernel<<<(uint32_t)chunks, 256, 0, s>>>(k, chunks);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_compact_move(const KvView& c, const KvLayers& l, const KvCompact& k, bool tables, int n_cu,
+                                  hipStream_t s) {
+    const int64_t work = std::max<int64_t>(k.entries, k.n_pages / 2);
+    const uint32_t table_groups = tables ? (uint32_t)std::min<int64_t>((work + 255) / 256, n_cu) : 0;
+    compact_move_kernel<<<table_groups + (uint32_t)n_cu * 8, 256, 0, s>>>(c, l, k, table_groups, k.counts + chunks_of(k.n_pages));
+    return hipGetLastError();
+}
+
+}  // namespace ls

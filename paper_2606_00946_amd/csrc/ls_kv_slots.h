@@ -44,4 +44,29 @@ constexpr TileRows tile_rows(int64_t i, int32_t n, int32_t G, int32_t tile) {
     return {r0, (int32_t)least(left, tile)};
 }
 
+// A tree's parts, `pairs` of (head, piece) for each of `tiles` row tiles: eight pairs beside
+// each other, then their next tile, so that the tiles that read the same codes run on one
+// XCD (workgroups go round eight) at about one time.
+struct TreePlace {
+    uint32_t pair, tile;
+};
+constexpr TreePlace tree_place(uint32_t at, uint32_t pairs, uint32_t tiles) {
+    const uint32_t even = pairs & ~7u;
+    if (at < even * tiles) return {at / (8 * tiles) * 8 + (at & 7), at % (8 * tiles) >> 3};
+    const uint32_t r = at - even * tiles, w = pairs - even;
+    return {even + r % w, r / w};
+}
+
+// The first n of 16 bits.
+constexpr uint32_t first_bits(int32_t n) { return n >= 16 ? 0xFFFFu : n <= 0 ? 0u : (1u << n) - 1; }
+
+// Which of the 16 tokens of a block a drafted row sees.  The block starts `rel` tokens after the
+// cached ones (before them: below 0); cached tokens i count unless i < gone and i >= sink, new ones by
+// the mask, whose words rel >> 6 and the next are lo and hi, up to the n-th.
+constexpr uint32_t tree_bits(int32_t rel, int32_t n, int32_t gone, int32_t sink, uint64_t lo, uint64_t hi) {
+    const uint32_t cached = first_bits(rel > 0 ? 0 : -(rel < -16 ? -16 : rel)), s = (uint32_t)rel & 63;
+    const uint64_t bits = lo >> s | (s ? hi << (64 - s) : 0);
+    return (cached & (~first_bits(gone) | first_bits(sink))) | ((uint32_t)bits & first_bits(n - rel) & ~cached);
+}
+
 }  // namespace ls

@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "ls_internal.h"
+#include "ls_kv_calls.h"
 #include "ls_scratch.h"
 #include "k_policy.h"
 
@@ -280,11 +281,13 @@ int grow(ls_ctx* c, void** p, size_t* cap, size_t bytes, hipStream_t s) {
 
 enum Kind {
     K_TABLE = 0, K_PREFIX, K_PARTIAL, K_SCORE, K_ARGMIN, K_UPDATE, K_SCORE_MFMA, K_BAND, K_RESCORE, K_ROUTE, K_BUFFER,
-    K_INDEX, K_KV_APPEND, K_KV_ATTENTION, K_KV_READ, K_COUNT
+    K_INDEX, K_KV_APPEND, K_KV_ATTENTION, K_KV_READ, K_KV_TREE, K_KV_KEEP,
+    K_KV_FORK, K_KV_COMPACT, K_COUNT
 };
 const char* const kKindNames[K_COUNT] = {"table_build", "prefix_match", "instance_partial", "score_pairs", "argmin",
                                          "update", "score_pairs_mfma", "band_select", "rescore", "route",
-                                         "buffer", "index", "kv_append", "kv_attention", "kv_read"};
+                                         "buffer", "index", "kv_append", "kv_attention", "kv_read",
+                                         "kv_tree", "kv_keep", "kv_fork", "kv_compact"};
 
 hipEvent_t take_event(ls_ctx* c) {
     if (!c->spare.empty()) {
@@ -1361,13 +1364,10 @@ namespace {
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
-// Checks the descriptors every KV call takes and turns them into the kernels' view.
-int kv_view(ls_ctx* c, const ls_kv_cache* kv, const ls_kv_batch* b, ls::KvView* out) {
-    if (!kv || !b) return fail(c, LS_ERR_INVALID, "cache and batch must be non-NULL");
+// A cache's descriptor, and the part of the kernels' view that it gives.
+int kv_cache(ls_ctx* c, const ls_kv_cache* kv, ls::KvView* v) {
     if (kv->dtype != LS_KV_INT8 && kv->dtype != LS_KV_FP8)
         return fail(c, LS_ERR_INVALID, "cache dtype must be LS_KV_INT8 or LS_KV_FP8");
-    if (b->dtype != LS_BF16 && b->dtype != LS_FP16)
-        return fail(c, LS_ERR_INVALID, "batch dtype must be LS_BF16 or LS_FP16");
     if (kv->n_kv_heads < 1 || kv->n_kv_heads > 1024) return fail(c, LS_ERR_INVALID, "n_kv_heads must be 1..1024");
     if (kv->head_dim != 64 && kv->head_dim != 128 && kv->head_dim != 256)
         return fail(c, LS_ERR_INVALID, "head_dim must be 64, 128 or 256");
@@ -1377,6 +1377,27 @@ int kv_view(ls_ctx* c, const ls_kv_cache* kv, const ls_kv_batch* b, ls::KvView* 
     if (!kv->k || !kv->v || !kv->k_scale || !kv->v_scale)
         return fail(c, LS_ERR_INVALID, "the cache's arrays must be non-NULL");
     if (!aligned16(kv->k) || !aligned16(kv->v)) return fail(c, LS_ERR_INVALID, "k and v must be 16-byte aligned");
+    v->k = (uint8_t*)kv->k;
+    v->v = (uint8_t*)kv->v;
+    v->ks = kv->k_scale;
+    v->vs = kv->v_scale;
+    v->n_pages = kv->n_pages;
+    v->H = kv->n_kv_heads;
+    v->D = kv->head_dim;
+    v->page = kv->page_tokens;
+    v->page_shift = __builtin_ctz((unsigned)kv->page_tokens);
+    v->fp8 = kv->dtype == LS_KV_FP8;
+    return LS_OK;
+}
+
+// Checks the descriptors that a call on one layer's cache takes (`tensors`: it has 16-bit ones) and turns them into the
+// kernels' view.
+int kv_view(ls_ctx* c, const ls_kv_cache* kv, const ls_kv_batch* b, ls::KvView* out, bool tensors = true) {
+    if (!kv || !b) return fail(c, LS_ERR_INVALID, "cache and batch must be non-NULL");
+    ls::KvView v;
+    if (int rc = kv_cache(c, kv, &v)) return rc;
+    if (tensors && b->dtype != LS_BF16 && b->dtype != LS_FP16)
+        return fail(c, LS_ERR_INVALID, "batch dtype must be LS_BF16 or LS_FP16");
     if (b->n_seqs < 0 || b->n_tokens < 0) return fail(c, LS_ERR_INVALID, "n_seqs and n_tokens must be >= 0");
     if (b->n_seqs > 0 && b->n_tokens > 0) {
         if (!b->new_off || !b->past || !b->pages)
@@ -1387,16 +1408,6 @@ int kv_view(ls_ctx* c, const ls_kv_cache* kv, const ls_kv_batch* b, ls::KvView* 
         if ((int64_t)b->pages_stride * kv->page_tokens > 1 << 30)
             return fail(c, LS_ERR_INVALID, "pages_stride * page_tokens must be at most 2^30");
     }
-    ls::KvView v;
-    v.k = (uint8_t*)kv->k;
-    v.v = (uint8_t*)kv->v;
-    v.ks = kv->k_scale;
-    v.vs = kv->v_scale;
-    v.n_pages = kv->n_pages;
-    v.H = kv->n_kv_heads;
-    v.D = kv->head_dim;
-    v.page = kv->page_tokens;
-    v.page_shift = __builtin_ctz((unsigned)kv->page_tokens);
     v.off = b->new_off;
     v.past = b->past;
     v.pages = b->pages;
@@ -1405,7 +1416,6 @@ int kv_view(ls_ctx* c, const ls_kv_cache* kv, const ls_kv_batch* b, ls::KvView* 
     v.W = b->pages_stride;
     v.max_new = std::min(b->max_new, b->n_tokens);
     v.limit = (int32_t)((int64_t)b->pages_stride * kv->page_tokens);
-    v.fp8 = kv->dtype == LS_KV_FP8;
     v.f16 = b->dtype == LS_FP16;
     *out = v;
     return LS_OK;
@@ -1426,21 +1436,71 @@ int kv_q_heads(ls_ctx* c, int32_t Hq, int32_t H) {
     return LS_OK;
 }
 
+// The caches of several layers: alike, the first one's view.
+int kv_layers(ls_ctx* c, const ls_kv_cache* caches, int32_t n, ls::KvView* v) {
+    if (!caches || n < 1) return fail(c, LS_ERR_INVALID, "caches must be non-NULL and n_caches >= 1");
+    for (int32_t i = n - 1; i >= 0; --i) {
+        if (int rc = kv_cache(c, &caches[i], v)) return rc;
+        const ls_kv_cache &a = caches[0], &b = caches[i];
+        if (a.dtype != b.dtype || a.n_kv_heads != b.n_kv_heads || a.head_dim != b.head_dim ||
+            a.page_tokens != b.page_tokens || a.n_pages != b.n_pages)
+            return fail(c, LS_ERR_INVALID, "the caches must have the same dtype, heads, dimensions, page tokens and pages");
+    }
+    return LS_OK;
+}
+
+// Calls f with the arrays of up to kMaxLayers caches at a time; whether they are the first.
+template <class F>
+hipError_t kv_by_layers(const ls_kv_cache* caches, int32_t n, F f) {
+    for (int32_t i0 = 0; i0 < n; i0 += ls::kMaxLayers) {
+        ls::KvLayers l{};
+        l.n = std::min(n - i0, ls::kMaxLayers);
+        for (int32_t i = 0; i < l.n; ++i) {
+            l.codes[0][i] = (uint8_t*)caches[i0 + i].k;
+            l.codes[1][i] = (uint8_t*)caches[i0 + i].v;
+            l.scales[0][i] = caches[i0 + i].k_scale;
+            l.scales[1][i] = caches[i0 + i].v_scale;
+        }
+        const hipError_t e = f(l, i0 == 0);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+// A page table: rows x stride entries.
+int kv_table(ls_ctx* c, const ls::KvView& v, int32_t rows, int32_t stride) {
+    if (rows < 0) return fail(c, LS_ERR_INVALID, "n_rows must be >= 0");
+    if (stride < 1) return fail(c, LS_ERR_INVALID, "pages_stride must be >= 1");
+    if ((int64_t)stride * v.page > 1 << 30)
+        return fail(c, LS_ERR_INVALID, "pages_stride * page_tokens must be at most 2^30");
+    return LS_OK;
+}
+
+// The workspace of `call`, allocated and its counts cleared by the context's first call that needs it.
+int kv_workspace(ls_ctx* c, const char* call, hipStream_t s) {
+    if (c->kv_ws_ready) return LS_OK;
+    // a capture would record the allocation and the clearing instead: the memory would be the graph's, the counts not clear
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    const hipError_t e = hipStreamIsCapturing(s, &capture);
+    if (e != hipSuccess) (void)hipGetLastError();
+    if (e != hipSuccess || capture != hipStreamCaptureStatusNone)
+        return fail(c, LS_ERR_STATE, "a context's first %s allocates its workspace: make one call before capturing", call);
+    if (int rc = grow(c, &c->kv_ws, &c->kv_ws_cap, LS_KV_WORKSPACE_BYTES, s)) return rc;
+    LS_HIP(c, ls::launch_kv_workspace_init(c->kv_ws, s));
+    c->kv_ws_ready = true;
+    return LS_OK;
+}
+
 int kv_launched(ls_ctx* c, hipError_t e) {
     if (e == hipErrorInvalidConfiguration) return fail(c, LS_ERR_UNSUPPORTED, "the batch is too large for one launch");
     LS_HIP(c, e);
     return LS_OK;
 }
 
-}  // namespace
-
-extern "C" {
-
-int ls_kv_append(ls_ctx* c, const ls_kv_cache* cache, const ls_kv_batch* batch, const ls_rope* rope, const void* k,
-                 int64_t k_stride, const void* v, int64_t v_stride, const void* q, int64_t q_stride,
-                 int32_t n_q_heads, void* q_out, int64_t q_out_stride, void* stream) {
-    if (!c) return LS_ERR_INVALID;
-    c->err.clear();
+// ls_kv_append, and with `positions` ls_kv_append_at.
+int kv_append(ls_ctx* c, const ls_kv_cache* cache, const ls_kv_batch* batch, const ls_rope* rope,
+              const ls_positions* positions, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+              const void* q, int64_t q_stride, int32_t n_q_heads, void* q_out, int64_t q_out_stride, hipStream_t s) {
     ls::KvView w;
     int rc = kv_view(c, cache, batch, &w);
     if (rc) return rc;
@@ -1454,6 +1514,20 @@ int ls_kv_append(ls_ctx* c, const ls_kv_cache* cache, const ls_kv_batch* batch, 
             return fail(c, LS_ERR_INVALID, "rotary must be a multiple of 32 in [32, head_dim]");
         r = {rope->cos_tab, rope->sin_tab, rope->n_positions, rope->rotary, rope->interleaved};
     }
+    ls::KvPositions at{};
+    if (positions) {
+        if (positions->n_axes < 1 || positions->n_axes > LS_MAX_AXES)
+            return fail(c, LS_ERR_INVALID, "n_axes must be 1..%d", LS_MAX_AXES);
+        if (w.T > 0 && !positions->pos) return fail(c, LS_ERR_INVALID, "pos must be non-NULL");
+        at.pos = positions->pos;
+        at.n_axes = positions->n_axes;
+        for (int32_t i = 0; positions->axis && i < r.rotary / 2; ++i) {
+            if (positions->axis[i] >= at.n_axes)
+                return fail(c, LS_ERR_INVALID, "axis[%d] is %d, outside [0, %d)", i, positions->axis[i], at.n_axes);
+            at.axis[i / 16] |= (uint32_t)positions->axis[i] << 2 * (i % 16);
+            at.mixed |= positions->axis[i] != positions->axis[i & ~7];
+        }
+    }
     if ((q == nullptr) != (q_out == nullptr)) return fail(c, LS_ERR_INVALID, "q and q_out go together");
     if (q && (rc = kv_q_heads(c, n_q_heads, w.H))) return rc;
     if (w.B == 0 || w.T == 0) return LS_OK;
@@ -1463,13 +1537,36 @@ int ls_kv_append(ls_ctx* c, const ls_kv_cache* cache, const ls_kv_batch* batch, 
         return rc;
     DeviceScope dev(c->device);
     if (!dev.ok) return fail(c, LS_ERR_DEVICE, "cannot select device %d", c->device);
-    hipStream_t s = (hipStream_t)stream;
     Timed t(c, K_KV_APPEND, s);
     const hipError_t e =
-        ls::launch_kv_append(w, r, k, k_stride, v, v_stride, q, q_stride, n_q_heads, q_out, q_out_stride,
-                             c->n_cu, s);
+        ls::launch_kv_append_at(w, r, at, k, k_stride, v, v_stride, q, q_stride, n_q_heads, q_out, q_out_stride,
+                                c->n_cu, s);
     t.done();
     return kv_launched(c, e);
+}
+
+}  // namespace
+
+extern "C" {
+
+int ls_kv_append(ls_ctx* c, const ls_kv_cache* cache, const ls_kv_batch* batch, const ls_rope* rope, const void* k,
+                 int64_t k_stride, const void* v, int64_t v_stride, const void* q, int64_t q_stride,
+                 int32_t n_q_heads, void* q_out, int64_t q_out_stride, void* stream) {
+    if (!c) return LS_ERR_INVALID;
+    c->err.clear();
+    return kv_append(c, cache, batch, rope, nullptr, k, k_stride, v, v_stride, q, q_stride, n_q_heads, q_out,
+                     q_out_stride, (hipStream_t)stream);
+}
+
+int ls_kv_append_at(ls_ctx* c, const ls_kv_cache* cache, const ls_kv_batch* batch, const ls_rope* rope,
+                    const ls_positions* positions, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                    const void* q, int64_t q_stride, int32_t n_q_heads, void* q_out, int64_t q_out_stride,
+                    void* stream) {
+    if (!c) return LS_ERR_INVALID;
+    c->err.clear();
+    if (!rope || !positions) return fail(c, LS_ERR_INVALID, "rope and positions must be non-NULL");
+    return kv_append(c, cache, batch, rope, positions, k, k_stride, v, v_stride, q, q_stride, n_q_heads, q_out,
+                     q_out_stride, (hipStream_t)stream);
 }
 
 int ls_kv_attention(ls_ctx* c, const ls_kv_cache* cache, const ls_kv_batch* batch, const void* q, int64_t q_stride,
@@ -1489,18 +1586,7 @@ int ls_kv_attention(ls_ctx* c, const ls_kv_cache* cache, const ls_kv_batch* batc
     DeviceScope dev(c->device);
     if (!dev.ok) return fail(c, LS_ERR_DEVICE, "cannot select device %d", c->device);
     hipStream_t s = (hipStream_t)stream;
-    if (!c->kv_ws_ready) {
-        // a capture would record the allocation and the clearing instead: the memory would be the graph's, the counts not clear
-        hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-        const hipError_t e = hipStreamIsCapturing(s, &capture);
-        if (e != hipSuccess) (void)hipGetLastError();
-        if (e != hipSuccess || capture != hipStreamCaptureStatusNone)
-            return fail(c, LS_ERR_STATE, "a context's first ls_kv_attention allocates its workspace: make one call before "
-                                         "capturing");
-        if ((rc = grow(c, &c->kv_ws, &c->kv_ws_cap, LS_KV_WORKSPACE_BYTES, s))) return rc;
-        LS_HIP(c, ls::launch_kv_workspace_init(c->kv_ws, s));
-        c->kv_ws_ready = true;
-    }
+    if ((rc = kv_workspace(c, "ls_kv_attention", s))) return rc;
     Timed t(c, K_KV_ATTENTION, s);
     const hipError_t e = ls::launch_kv_attention(w, q, q_stride, n_q_heads, scale, window, sinks, out, out_stride,
                                                  c->kv_ws, (int64_t)c->kv_ws_cap, c->n_cu, s);
@@ -1524,6 +1610,108 @@ int ls_kv_read(ls_ctx* c, const ls_kv_cache* cache, const ls_kv_batch* batch, vo
     hipStream_t s = (hipStream_t)stream;
     Timed t(c, K_KV_READ, s);
     const hipError_t e = ls::launch_kv_read(w, k_out, v_out, s);
+    t.done();
+    return kv_launched(c, e);
+}
+
+int ls_kv_attention_tree(ls_ctx* c, const ls_kv_cache* cache, const ls_kv_batch* batch, const ls_tree* tree,
+                         const void* q, int64_t q_stride, int32_t n_q_heads, float scale, int32_t window, int32_t sinks,
+                         void* out, int64_t out_stride, void* stream) {
+    if (!c) return LS_ERR_INVALID;
+    c->err.clear();
+    if (!tree) return fail(c, LS_ERR_INVALID, "tree must be non-NULL");
+    ls::KvView w;
+    int rc = kv_view(c, cache, batch, &w);
+    if (rc || (rc = kv_q_heads(c, n_q_heads, w.H))) return rc;
+    if (!std::isfinite(scale)) return fail(c, LS_ERR_INVALID, "scale must be finite");
+    if (window < 0 || sinks < 0) return fail(c, LS_ERR_INVALID, "window and sinks must be >= 0");
+    if (w.B == 0 || w.T == 0) return LS_OK;
+    if (!tree->mask) return fail(c, LS_ERR_INVALID, "mask must be non-NULL");
+    if ((int64_t)tree->mask_words * 64 < w.max_new)
+        return fail(c, LS_ERR_INVALID, "mask_words must hold max_new bits");
+    if (window > 0 && !tree->pos) return fail(c, LS_ERR_INVALID, "a window needs the rows' positions");
+    if ((rc = kv_tensor(c, "q", q, q_stride, n_q_heads, w.D)) ||
+        (rc = kv_tensor(c, "out", out, out_stride, n_q_heads, w.D)))
+        return rc;
+    DeviceScope dev(c->device);
+    if (!dev.ok) return fail(c, LS_ERR_DEVICE, "cannot select device %d", c->device);
+    hipStream_t s = (hipStream_t)stream;
+    if ((rc = kv_workspace(c, "ls_kv_attention_tree", s))) return rc;
+    Timed t(c, K_KV_TREE, s);
+    const hipError_t e = ls::launch_kv_tree(w, {tree->mask, tree->mask_words, tree->pos}, q, q_stride, n_q_heads, scale,
+                                            window, sinks, out, out_stride, c->kv_ws, (int64_t)c->kv_ws_cap, c->n_cu, s);
+    t.done();
+    return kv_launched(c, e);
+}
+
+int ls_kv_keep(ls_ctx* c, const ls_kv_cache* caches, int32_t n_caches, const ls_kv_batch* batch, const int32_t* kept,
+               const int32_t* n_kept, void* stream) {
+    if (!c) return LS_ERR_INVALID;
+    c->err.clear();
+    ls::KvView w;
+    int rc = kv_layers(c, caches, n_caches, &w);
+    if (rc || (rc = kv_view(c, caches, batch, &w, false))) return rc;
+    if (w.B == 0 || w.T == 0) return LS_OK;
+    if (!kept || !n_kept) return fail(c, LS_ERR_INVALID, "kept and n_kept must be non-NULL");
+    DeviceScope dev(c->device);
+    if (!dev.ok) return fail(c, LS_ERR_DEVICE, "cannot select device %d", c->device);
+    hipStream_t s = (hipStream_t)stream;
+    Timed t(c, K_KV_KEEP, s);
+    const hipError_t e = kv_by_layers(caches, n_caches, [&](const ls::KvLayers& l, bool) {
+        return ls::launch_kv_keep(w, l, kept, n_kept, s);
+    });
+    t.done();
+    return kv_launched(c, e);
+}
+
+int ls_kv_fork(ls_ctx* c, const ls_kv_cache* caches, int32_t n_caches, int32_t n_rows, int32_t pages_stride,
+               const int32_t* pages, int32_t* pages_out, int32_t n_forks, const int32_t* src, const int32_t* dst,
+               const int32_t* tokens, void* stream) {
+    if (!c) return LS_ERR_INVALID;
+    c->err.clear();
+    ls::KvView w{};
+    int rc = kv_layers(c, caches, n_caches, &w);
+    if (rc || (rc = kv_table(c, w, n_rows, pages_stride))) return rc;
+    if (n_forks < 0) return fail(c, LS_ERR_INVALID, "n_forks must be >= 0");
+    if (n_forks == 0 || n_rows == 0) return LS_OK;
+    if (!pages || !pages_out || !src || !dst || !tokens)
+        return fail(c, LS_ERR_INVALID, "pages, pages_out, src, dst and tokens must be non-NULL");
+    DeviceScope dev(c->device);
+    if (!dev.ok) return fail(c, LS_ERR_DEVICE, "cannot select device %d", c->device);
+    hipStream_t s = (hipStream_t)stream;
+    const ls::KvForks f = {pages, pages_out, n_rows, pages_stride, n_forks, src, dst, tokens};
+    Timed t(c, K_KV_FORK, s);
+    const hipError_t e = kv_by_layers(caches, n_caches, [&](const ls::KvLayers& l, bool first) {
+        return ls::launch_kv_fork(w, l, f, first, s);
+    });
+    t.done();
+    return kv_launched(c, e);
+}
+
+int ls_kv_compact(ls_ctx* c, const ls_kv_cache* caches, int32_t n_caches, int32_t n_rows, int32_t pages_stride,
+                  const int32_t* pages, int32_t* pages_out, int32_t* where, int32_t* n_used, void* stream) {
+    if (!c) return LS_ERR_INVALID;
+    c->err.clear();
+    ls::KvView w{};
+    int rc = kv_layers(c, caches, n_caches, &w);
+    if (rc || (rc = kv_table(c, w, n_rows, pages_stride))) return rc;
+    if (!where || !n_used || (n_rows > 0 && (!pages || !pages_out)))
+        return fail(c, LS_ERR_INVALID, "pages, pages_out, where and n_used must be non-NULL");
+    if (ls::kv_compact_bytes(w.n_pages) > (int64_t)LS_KV_WORKSPACE_BYTES - ls::kKvCountBytes)
+        return fail(c, LS_ERR_UNSUPPORTED, "the workspace holds the moves of a pool of up to 16 million pages");
+    DeviceScope dev(c->device);
+    if (!dev.ok) return fail(c, LS_ERR_DEVICE, "cannot select device %d", c->device);
+    hipStream_t s = (hipStream_t)stream;
+    if ((rc = kv_workspace(c, "ls_kv_compact", s))) return rc;
+    ls::KvCompact k{pages, pages_out, (int64_t)n_rows * pages_stride, where, n_used, (int32_t)w.n_pages, nullptr, nullptr, nullptr};
+    // behind the counts that attention keeps at zero
+    ls::kv_compact_carve(k, (char*)c->kv_ws + ls::kKvCountBytes);
+    Timed t(c, K_KV_COMPACT, s);
+    hipError_t e = ls::launch_kv_compact_plan(k, c->n_cu, s);
+    if (e == hipSuccess)
+        e = kv_by_layers(caches, n_caches, [&](const ls::KvLayers& l, bool first) {
+            return ls::launch_kv_compact_move(w, l, k, first, c->n_cu, s);
+        });
     t.done();
     return kv_launched(c, e);
 }

@@ -78,6 +78,14 @@ class ls_rope(ctypes.Structure):
                 ("rotary", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
 
 
+class ls_positions(ctypes.Structure):
+    _fields_ = [("n_axes", ctypes.c_int32), ("pos", ctypes.c_void_p), ("axis", ctypes.c_void_p)]
+
+
+class ls_tree(ctypes.Structure):
+    _fields_ = [("mask", ctypes.c_void_p), ("mask_words", ctypes.c_int32), ("pos", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -127,6 +135,12 @@ def library():
         lib.ls_kv_append.argtypes = [P, kvp, kbp, ctypes.POINTER(ls_rope), P, i64, P, i64, P, i64, i32, P, i64, P]
         lib.ls_kv_attention.argtypes = [P, kvp, kbp, P, i64, i32, f32, i32, i32, P, i64, P]
         lib.ls_kv_read.argtypes = [P, kvp, kbp, P, P, P]
+        lib.ls_kv_append_at.argtypes = [P, kvp, kbp, ctypes.POINTER(ls_rope), ctypes.POINTER(ls_positions), P, i64, P, i64,
+                                        P, i64, i32, P, i64, P]
+        lib.ls_kv_attention_tree.argtypes = [P, kvp, kbp, ctypes.POINTER(ls_tree), P, i64, i32, f32, i32, i32, P, i64, P]
+        lib.ls_kv_keep.argtypes = [P, kvp, i32, kbp, P, P, P]
+        lib.ls_kv_fork.argtypes = [P, kvp, i32, i32, i32, P, P, i32, P, P, P, P]
+        lib.ls_kv_compact.argtypes = [P, kvp, i32, i32, i32, P, P, P, P, P]
         for f in (lib.ls_create, lib.ls_set_model, lib.ls_get_model, lib.ls_load_cache_state, lib.ls_score_batch,
                   lib.ls_update, lib.ls_profile_enable, lib.ls_profile_read, lib.ls_set_exact_scores,
                   lib.ls_set_prefix_join, lib.ls_route_batch, lib.ls_set_prefix_closed, lib.ls_buffer_init,
@@ -134,7 +148,8 @@ def library():
                   lib.ls_set_cache_capacity, lib.ls_commit_routes, lib.ls_read_cache_state, lib.ls_set_dropout,
                   lib.ls_set_shadow_training, lib.ls_swap_model, lib.ls_fast_scores, lib.ls_set_cu_limit,
                   lib.ls_set_chain_kernels,
-                  lib.ls_score_batch_noalloc, lib.ls_kv_append, lib.ls_kv_attention, lib.ls_kv_read):
+                  lib.ls_score_batch_noalloc, lib.ls_kv_append, lib.ls_kv_attention, lib.ls_kv_read, lib.ls_kv_append_at,
+                  lib.ls_kv_attention_tree, lib.ls_kv_keep, lib.ls_kv_fork, lib.ls_kv_compact):
             f.restype = ctypes.c_int
         _lib = lib
     return _lib
@@ -251,6 +266,56 @@ class Rope:
         self.c = ls_rope(_dev(cos, "cos", (torch.float32,)), _dev(sin, "sin", (torch.float32,)), cos.shape[0],
                          2 * cos.shape[1], int(bool(interleaved)))
         self.ref = ctypes.byref(self.c)
+
+
+class Positions:
+    """Rows' positions on 1 to 4 axes (ls_positions): pos int32 [T] or [axes x T] on the device; axis, a host sequence
+    of rotary / 2 axis numbers, says by which one each rotary pair turns (default: all by the first)."""
+
+    def __init__(self, pos, axis=None):
+        import torch
+        if pos.dim() not in (1, 2):
+            raise ValueError("pos must be [T] or [axes x T]")
+        self.pos, self.n_tokens = pos, pos.shape[-1]
+        self.axis = None if axis is None else np.ascontiguousarray(axis, dtype=np.uint8)
+        if axis is not None and (self.axis.ndim != 1 or not np.array_equal(self.axis, axis)):
+            raise ValueError("axis must be one axis number for each rotary pair")
+        self.c = ls_positions(1 if pos.dim() == 1 else pos.shape[0], _dev(pos, "pos", (torch.int32,)),
+                              None if axis is None else self.axis.ctypes.data)
+        self.ref = ctypes.byref(self.c)
+
+
+class Tree:
+    """What drafted rows see (ls_tree): mask int64 [T x words] on the device, bit j of a row: it sees its sequence's new
+    token j; pos int32 [T], the rows' positions, needed with a window."""
+
+    def __init__(self, mask, pos=None):
+        import torch
+        if mask.dim() != 2:
+            raise ValueError("mask must be [T x words]")
+        self.mask, self.pos, self.n_tokens = mask, pos, mask.shape[0]
+        self.c = ls_tree(_dev(mask, "mask", (torch.int64, torch.uint64)), mask.shape[1],
+                         _dev(pos, "pos", (torch.int32,), mask.shape[0], True))
+        self.ref = ctypes.byref(self.c)
+
+
+class KVLayers:
+    """The caches of several layers, alike in all but their tensors, for the calls that take all of them."""
+
+    def __init__(self, caches):
+        self.caches = tuple(caches)
+        if not self.caches:
+            raise ValueError("at least one cache is needed")
+        self.c = (ls_kv_cache * len(self.caches))(*(x.c for x in self.caches))
+        self.ref, self.n = self.c, len(self.caches)
+        self.n_pages = int(self.c[0].n_pages)
+
+
+def _layers(caches):
+    """(pointer, number, pages) of a KVLayers, or of one KVCache."""
+    if isinstance(caches, KVCache):
+        return caches.ref, 1, int(caches.c.n_pages)
+    return caches.ref, caches.n, caches.n_pages
 
 
 _LS_16 = {}
@@ -584,6 +649,73 @@ class Context:
         kp, _, _ = _rows(k_out, "k_out", batch, D, H)
         vp, _, _ = _rows(v_out, "v_out", batch, D, H, k_out)
         return self._check("ls_kv_read", self.lib.ls_kv_read(self.h, cache.ref, batch.ref, kp, vp, _raw_stream(stream, self.device)))
+
+    def ls_kv_append_at(self, cache, batch, positions, k, v, rope, q=None, q_out=None, stream=None):
+        """ls_kv_append with keys and queries turned by positions (a Positions) instead of their places."""
+        D, H = cache.head_dim, cache.n_kv_heads
+        if positions.n_tokens != batch.n_tokens:
+            raise ValueError(f"positions are of {positions.n_tokens} rows, expected {batch.n_tokens}")
+        if positions.axis is not None and 2 * positions.axis.size != rope.c.rotary:
+            raise ValueError(f"axis has {positions.axis.size} numbers, expected {rope.c.rotary // 2}")
+        kp, ks, _ = _rows(k, "k", batch, D, H)
+        vp, vs, _ = _rows(v, "v", batch, D, H, k)
+        qp = op = None
+        qs = os_ = qh = 0
+        if q is not None or q_out is not None:
+            if q is None or q_out is None:
+                raise ValueError("q and q_out go together")
+            qp, qs, qh = _rows(q, "q", batch, D, like=k)
+            op, os_, _ = _rows(q_out, "q_out", batch, D, qh, k)
+        return self._check("ls_kv_append_at",
+                           self.lib.ls_kv_append_at(self.h, cache.ref, batch.ref, rope.ref, positions.ref, kp, ks, vp, vs,
+                                                    qp, qs, qh, op, os_, _raw_stream(stream, self.device)))
+
+    def ls_kv_attention_tree(self, cache, batch, tree, q, out, scale=None, window=0, sinks=0, stream=None):
+        """out [T x q heads x D]: attention of drafted rows over the cache and the drafts that tree (a Tree) shows them."""
+        D = cache.head_dim
+        if tree.n_tokens != batch.n_tokens:
+            raise ValueError(f"mask has {tree.n_tokens} rows, expected {batch.n_tokens}")
+        qp, qs, qh = _rows(q, "q", batch, D)
+        op, os_, _ = _rows(out, "out", batch, D, qh, q)
+        return self._check("ls_kv_attention_tree",
+                           self.lib.ls_kv_attention_tree(self.h, cache.ref, batch.ref, tree.ref, qp, qs, qh,
+                                                         D ** -0.5 if scale is None else scale, window, sinks, op, os_,
+                                                         _raw_stream(stream, self.device)))
+
+    def ls_kv_keep(self, caches, batch, kept, n_kept, stream=None):
+        """Keeps a path of each sequence's drafts in all layers (a KVLayers, or one KVCache): new token kept[new_off[b] + i]
+        becomes new token i for i < n_kept[b]; kept int32 [T], n_kept int32 [B] on the device."""
+        import torch
+        ref, n, _ = _layers(caches)
+        i32 = (torch.int32,)
+        return self._check("ls_kv_keep", self.lib.ls_kv_keep(
+            self.h, ref, n, batch.ref, _dev(kept, "kept", i32, batch.n_tokens), _dev(n_kept, "n_kept", i32, batch.c.n_seqs),
+            _raw_stream(stream, self.device)))
+
+    def ls_kv_fork(self, caches, pages, pages_out, src, dst, tokens, stream=None):
+        """Rows dst of pages_out take over the first tokens of rows src of pages (int32 [rows x stride], device); a partly
+        filled last page is copied, in all layers, onto the one that pages_out has there."""
+        import torch
+        ref, n, _ = _layers(caches)
+        i32 = (torch.int32,)
+        if pages.dim() != 2 or pages.shape != pages_out.shape:
+            raise ValueError("pages and pages_out must be [rows x stride], alike")
+        return self._check("ls_kv_fork", self.lib.ls_kv_fork(
+            self.h, ref, n, pages.shape[0], pages.shape[1], _dev(pages, "pages", i32), _dev(pages_out, "pages_out", i32),
+            src.numel(), _dev(src, "src", i32), _dev(dst, "dst", i32, src.numel()), _dev(tokens, "tokens", i32, src.numel()),
+            _raw_stream(stream, self.device)))
+
+    def ls_kv_compact(self, caches, pages, pages_out, where, n_used, stream=None):
+        """Moves the pages that a table names to the lowest ids, in all layers: pages_out gets the table's new ids, where
+        int32 [n_pages] every page's (-1: not named), n_used int32 [1] their number."""
+        import torch
+        ref, n, n_pages = _layers(caches)
+        i32 = (torch.int32,)
+        if pages.dim() != 2 or pages.shape != pages_out.shape:
+            raise ValueError("pages and pages_out must be [rows x stride], alike")
+        return self._check("ls_kv_compact", self.lib.ls_kv_compact(
+            self.h, ref, n, pages.shape[0], pages.shape[1], _dev(pages, "pages", i32), _dev(pages_out, "pages_out", i32),
+            _dev(where, "where", i32, n_pages), _dev(n_used, "n_used", i32, 1), _raw_stream(stream, self.device)))
 
     # -- per-kernel timing ------------------------------------------------
     def ls_profile_enable(self, enable=True):
