@@ -635,8 +635,8 @@ int ls_kv_read(ls_ctx* ctx, const ls_kv_cache* cache, const ls_kv_batch* batch, 
  *   all layers; past[b] grows by n_kept[b] afterwards (the caller's).  A list ascends; it ends before the first
  *   entry that does not, or is no new token of the sequence.  A token whose old or new page is absent
  *   stays where it is.  A page that tokens move into gets the larger of its scale and the one that the largest
- *   magnitude among them asks for (ls_kv_append's rule), and what it holds up to the last kept token is brought
- *   to it; codes are rounded once more where the scales differ.  What lies behind the last kept token is nobody's.
+ *   magnitude among them asks for (ls_kv_append's rule, the division by 127 as a product with 1 / 127 in fp32), and
+ *   what it holds up to the last kept token is brought to it; codes are rounded once more where the scales differ.  What lies behind the last kept token is nobody's.
  * ls_kv_fork  for i < n_forks, row dst[i] of pages_out takes over the first tokens[i] tokens of row src[i] of
  *   pages (tables int32 [n_rows x pages_stride]; src, dst, tokens int32 [n_forks], all on the device): entries of
  *   pages that these tokens fill are copied, so both rows share them; where the last page is only partly filled, its

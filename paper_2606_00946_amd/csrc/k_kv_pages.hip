@@ -51,6 +51,13 @@ __device__ __forceinline__ uint32_t regraded(uint32_t w, float again) {
     return codes_of<FP8>(f.x * again, f.y * again, f.z * again, f.w * again);
 }
 
+// The scale that a largest magnitude asks for; for int8 by one product with 1 / 127 as 32 bits
+// hold it, within 2^-23 of the quotient.
+template <bool FP8>
+__device__ __forceinline__ float kept_scale(float a) {
+    return FP8 ? scale_of<true>(a) : fminf(fmaxf(a * (1.0f / 127.0f), kScaleMin), kScaleMax);
+}
+
 // A wave: one layer's keys or values of a sequence and head.  Page by page, 16 tokens
 // at a time: a lane holds, of every 64 dimensions, 16 of one key, or four of each of four
 // values.  Once for the largest magnitude that moves in, once for the codes; a page of
@@ -114,7 +121,7 @@ __device__ __forceinline__ void keep_rows(const KvView& c, uint8_t* codes, float
             }
         }
         if (!any) continue;
-        const float scale = fmaxf(scale_of<FP8>(wave_max(top)), held), inv = 1.0f / scale;
+        const float scale = fmaxf(kept_scale<FP8>(wave_max(top)), held), inv = 1.0f / scale;
         int loaded = b1 - 1;
         for (int blk = scale > held ? 0 : b0; blk < b1; ++blk) {
             if (blk != loaded) load(blk);

@@ -7,10 +7,10 @@
 //
 // A tree's rows (new tokens x query heads of one kv head) are more than a decode step's
 // and fewer than a prompt's, over as many cached tokens: at 4 D operations and 2 D
-// bytes a token, reading and computing take the same time at about 130 rows.  So the
-// tokens are what is dealt out: a wave takes 32 of a unit's 128 tokens with all of a
-// tile's 32 or 64 rows, codes go from memory to registers in 16-byte loads and each
-// operand made of them serves all rows.  Only the queries are in LDS.
+// bytes a token, reading and computing take the same time at about 130 rows.
+// So the tokens are what is dealt out: a wave takes 32 of a unit's 128 tokens with all
+// of a tile's 32 or 64 rows, codes go from memory to registers in 16-byte loads and
+// each operand made of them serves all rows; only the queries are in LDS.
 #include <algorithm>
 
 #include "k_kv_attend.h"
@@ -26,6 +26,8 @@ struct TreeArgs : AttnArgs {
     const uint64_t* mask;
     int32_t words;
     const int32_t* pos;
+    int32_t fit;                     // workgroups that fit the device
+    int64_t groups;                  // no more have work
 };
 
 static_assert(kMaxParts * 2 * 4 == kKvCountBytes, "the counts' part of the workspace");
@@ -59,6 +61,13 @@ __device__ __forceinline__ uint32_t tree_sight(const TreeArgs& a, const uint64_t
     return tree_bits(rel, n, gone, a.sinks - tok, lo, hi);
 }
 
+// A value as of this place: what is made of it is not computed ahead, to be kept in registers
+// (or in memory, which costs microseconds) through all that comes before.
+__device__ __forceinline__ int here(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 // Four bits as bytes.
 __device__ __forceinline__ uint32_t bytes_of(uint32_t four) { return ((four & 15u) * 0x00204081u & 0x01010101u) * 0xFFu; }
 
@@ -81,77 +90,164 @@ struct TreeLds {
     float undo[ROWS];                        // what undoes a row's scaling
 };
 
-template <int D, bool FP8, int NR>
-__global__ __launch_bounds__(256, 2) void kv_tree_kernel(KvView c, TreeArgs a, bool cut) {
-    constexpr int ROWS = 32 * NR, ND = D / 64, NC = D / 32;
-    __shared__ TreeLds<D, NR> lds;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col = lane & 31, hi = lane >> 5;
+// A lane's value for the whole wave.
+__device__ __forceinline__ int64_t of_lane64(int64_t x, int l) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, l));
+}
 
-    // Segments (sequence, head, row tile) are cut into equal parts of at most `most` units, so that about as many parts
-    // as workgroups hold all units (not cut: a part is a segment).
-    uint32_t most = 1u << 30;
-    TreeSeq mine = {0, 0, 0, 0, 0};          // of the first 64 sequences, a lane each
-    if (lane < c.B) mine = tree_seq<ROWS>(c, a, lane);
-    if (cut) {
-        uint64_t all = 0, segs = 0;
-        for (int b0 = 0; b0 < c.B; b0 += 64) {
-            TreeSeq s = mine;
-            if (b0 > 0) {
-                s.units = s.tiles = 0;
-                if (b0 + lane < c.B) s = tree_seq<ROWS>(c, a, b0 + lane);
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o);
+    return x;
+}
+
+// A workgroup's stretch of a sequence's line (tree_cut) for one row tile: a wave's copy in LDS, since there are no
+// registers to spare between its pieces.
+struct TreeStretch {
+    int32_t b, t0, n, past, units, r0;
+    int32_t stretch, first_group;        // the stretch, and the first workgroup of this tile among those of cut lines
+    int32_t h;                           // the head that is next
+    int32_t per, hi;                     // stretches' length; the stretch's end
+};
+
+constexpr int kTries = 6;
+
+// The piece at hand.
+template <int ROWS>
+struct TreeWork {
+    const KvView& c;
+    const TreeArgs& a;
+    TreeStretch& kept;
+    int b, h, t0, n, r0, rows, u0, u1;
+    int32_t past;
+
+    // The index-th workgroup's; whether it has one.  Stretches are as long as lets all workgroups that fit the device have
+    // one and no more (a line's last stretch costs up to a whole one more: how much of one on average is tried); where
+    // there are more tiles than that, long lines are still cut, into stretches twice what each workgroup would have.
+    __device__ __forceinline__ bool find(int64_t index) {
+        const int lane = here(threadIdx.x & 63);
+        auto seq_at = [&](int b) { return b < c.B ? tree_seq<ROWS>(c, a, b) : TreeSeq{0, 0, 0, 0, 0}; };
+        const TreeSeq early = seq_at(lane);          // of the first 64 sequences, a lane each
+        const float fit = (float)a.fit;
+        float all = 0.0f, each = 0.0f, tiles = 0.0f;
+        bool found = false;
+        // first the sums, then some tries, then the workgroup's place; one body for all: the code's own length is what it
+        // costs
+#pragma clang loop unroll(disable)
+        for (int pass = 0;; ++pass) {
+            int64_t groups = 0, cut = 0;             // workgroups, and those of cut lines
+#pragma clang loop unroll(disable)
+            for (int b0 = 0; b0 < c.B; b0 += 64) {
+                const TreeSeq s = b0 == 0 ? early : seq_at(b0 + lane);
+                const int32_t length = (s.units + kTreeStart) * c.H;
+                if (pass == 0) all += wave_sum((float)length * (float)s.tiles);
+                const int32_t want = max((int32_t)fminf(ceilf((float)length / each), fit), 1);
+                const int32_t per = pass == 0 ? length : tree_stretch(s.units, c.H, want);
+                const int32_t w = (int32_t)((uint32_t)(length + per - 1) / (uint32_t)per), mine = w * s.tiles;
+                const int32_t upto = (int32_t)wave_scan((uint32_t)mine), cuts = (int32_t)wave_scan(w > 1 ? (uint32_t)mine : 0u);
+                const uint64_t here_it_is = found ? __ballot(groups + upto > index) : 0;
+                if (here_it_is) {
+                    const int k = __ffsll((long long)here_it_is) - 1;
+                    TreeStretch x;
+                    x.b = b0 + k;
+                    x.t0 = __builtin_amdgcn_readlane(s.t0, k);
+                    x.n = __builtin_amdgcn_readlane(s.n, k);
+                    x.past = __builtin_amdgcn_readlane(s.past, k);
+                    x.units = __builtin_amdgcn_readlane(s.units, k);
+                    const int32_t all_w = __builtin_amdgcn_readlane(w, k), its = __builtin_amdgcn_readlane(s.tiles, k);
+                    const TreePlace p =
+                        tree_place((int32_t)(index - groups) - (__builtin_amdgcn_readlane(upto, k) - all_w * its), all_w, its);
+                    x.r0 = p.tile * ROWS;
+                    x.stretch = p.stretch;
+                    x.first_group = (int32_t)cut + __builtin_amdgcn_readlane(cuts, k) - all_w * its + p.tile * all_w;
+                    x.per = __builtin_amdgcn_readlane(per, k);
+                    x.hi = (int32_t)min((int64_t)(p.stretch + 1) * x.per, (int64_t)__builtin_amdgcn_readlane(length, k));
+                    x.h = (int32_t)((uint32_t)p.stretch * (uint32_t)x.per / (uint32_t)(x.units + kTreeStart));
+                    kept = x;
+                    return true;
+                }
+                groups += __builtin_amdgcn_readlane(upto, 63);
+                cut += __builtin_amdgcn_readlane(cuts, 63);
             }
-            const uint64_t x = (uint64_t)s.units * s.tiles;
-            // below 2^23 units, and 2^30 rows of a call: sums of 64 in two halves
-            all += __builtin_amdgcn_readlane(wave_scan((uint32_t)(x & 0xFFFFFu)), 63) +
-                   ((uint64_t)__builtin_amdgcn_readlane(wave_scan((uint32_t)(x >> 20 & 0xFFFFFu)), 63) << 20) +
-                   ((uint64_t)__builtin_amdgcn_readlane(wave_scan((uint32_t)(x >> 40)), 63) << 40);
-            segs += __builtin_amdgcn_readlane(wave_scan((uint32_t)s.tiles), 63);
+            if (found) return false;
+            if (pass == 0) {
+                tiles = (float)groups;
+            } else if ((pass <= kTries ? groups : cut) <= a.fit) {
+                found = true;
+                continue;
+            }
+            if (pass < kTries) {
+                each = all / fmaxf(fit - tiles * (0.3f + 0.7f / (kTries - 1) * (float)pass), 0.0f);
+            } else if (pass == kTries) {
+                each = 2.0f * all / fit;
+            } else {
+                each = INFINITY;                     // nothing is cut
+                found = true;
+            }
         }
-        const uint64_t room = max((int64_t)gridDim.x - (int64_t)(segs * (uint32_t)c.H), (int64_t)1);
-        const uint64_t each = (all * (uint32_t)c.H + room - 1) / room;
-        most = (uint32_t)min(max(each, (uint64_t)kMinUnits), (uint64_t)1 << 30);
     }
-    for (uint64_t part = blockIdx.x;; part += gridDim.x) {
-        // sequences' first parts are the sums of the parts before them
-        uint64_t base = 0;
-        uint32_t own = 0, count = 0, before = 0;
-        uint64_t found = 0;
-        TreeSeq its = mine;
-        int b0 = 0;
-        for (; b0 < c.B; b0 += 64) {
-            if (b0 > 0) {
-                its = TreeSeq{0, 0, 0, 0, 0};
-                if (b0 + lane < c.B) its = tree_seq<ROWS>(c, a, b0 + lane);
-            }
-            own = ((uint32_t)its.units + most - 1) / most;
-            count = own * (uint32_t)its.tiles * (uint32_t)c.H;
-            before = wave_scan(count);
-            found = __ballot(base + before > part);
-            if (found) break;
-            base += __builtin_amdgcn_readlane(before, 63);
+    // The next piece; whether there is one.
+    __device__ __forceinline__ bool next() {
+        const int32_t units = of(kept.units), lo = of(kept.stretch) * of(kept.per), hi = of(kept.hi);
+        for (h = of(kept.h);; ++h) {
+            const int32_t place = h * (units + kTreeStart);
+            if (place >= hi) return false;
+            u0 = tree_cut(lo - place, units);
+            u1 = place + units + kTreeStart <= hi ? units : tree_cut(hi - place, units);
+            if (u0 < u1) break;
         }
-        if (!found) return;
-        const int k = __ffsll((long long)found) - 1;
-        const int b = b0 + k;
-        const int t0 = __builtin_amdgcn_readlane(its.t0, k), n = __builtin_amdgcn_readlane(its.n, k);
-        const int32_t past = __builtin_amdgcn_readlane(its.past, k);
-        const int32_t units = __builtin_amdgcn_readlane(its.units, k);
-        const uint32_t tiles = __builtin_amdgcn_readlane(its.tiles, k);
-        const uint32_t pieces = __builtin_amdgcn_readlane(own, k);
-        const uint64_t start = base + __builtin_amdgcn_readlane(before - count, k);
-        const TreePlace place = tree_place((uint32_t)(part - start), pieces * (uint32_t)c.H, tiles);
-        const uint32_t pair = place.pair, tile = place.tile;
-        const int h = (int)(pair / pieces), piece = (int)(pair % pieces);
-        const uint64_t seg = start + ((uint64_t)h * tiles + tile) * pieces;     // the segment's first part as its sums lie
+        kept.h = h + 1;
+        b = of(kept.b);
+        t0 = of(kept.t0);
+        n = of(kept.n);
+        past = of(kept.past);
+        r0 = of(kept.r0);
+        rows = min(n * a.G - r0, ROWS);
+        return true;
+    }
+    static __device__ __forceinline__ int32_t of(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+    // Joins the head's pieces, where there are several: put(slot) writes the workgroup's sums, add(slot, first, step, n) makes
+    // them the sums of the pieces from `first` on, `step` apart, in their order.  Pieces are added in groups of
+    // kJoin: whoever finishes a group's last piece adds the group's pieces, whoever finishes the last group adds the
+    // groups' sums.  Whether the sums are the head's then.  A stretch has four counts: of the group that its piece inside
+    // a head leads, of the one that its piece at a head's start does, of that head's groups.
+    template <class Put, class Add>
+    __device__ __forceinline__ bool join(Put put, Add add) const {
+        const int32_t units = of(kept.units), stretch = of(kept.stretch);
+        if (u0 == 0 && u1 == units) return true;
+        const TreePieces range = tree_pieces(h * (units + kTreeStart), units, of(kept.per));
+        const int piece = (int)(stretch - range.first), pieces = (int)(range.last - range.first) + 1;
+        const int group = piece / kJoin, lead = group * kJoin, members = min(kJoin, pieces - lead), groups = (pieces - 1) / kJoin + 1;
+        const int32_t first = of(kept.first_group) + range.first;
+        auto slot = [&](int j) { return tree_slot(first, j); };
+        put(slot(piece));
+        if (!arrive(a.arrived + 4 * (first + lead) + (group == 0), members)) return false;
+        add(slot, lead, 1, members);
+        if (groups == 1) return true;
+        // the group's sum in the place of its first piece, which all of the workgroup has read
+        __syncthreads();
+        put(slot(lead));
+        if (!arrive(a.arrived + 4 * first + 2, groups)) return false;
+        add(slot, 0, kJoin, groups);
+        return true;
+    }
+};
 
+template <int D, bool FP8, int NR>
+__global__ __launch_bounds__(256, 2) void kv_tree_kernel(KvView c, TreeArgs a) {
+    constexpr int ROWS = 32 * NR, ND = D / 64, NC = D / 32;
+    constexpr bool HELD = D * NR <= 128;
+    constexpr int DEPTH = D * NR <= 128 ? 2 : 1;         // steps whose codes are on their way
+    __shared__ TreeLds<D, NR> lds;
+    __shared__ TreeStretch stretch[4];
+    TreeWork<ROWS> work{c, a, stretch[__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)]};
+    for (int64_t i = blockIdx.x; i < a.groups && work.find(i); i += gridDim.x) while (work.next()) {
+        const int thread = here(threadIdx.x), lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+        const int col = lane & 31, hi = lane >> 5;
+        const int b = work.b, h = work.h, t0 = work.t0, n = work.n, r0 = work.r0, rows = work.rows, u0 = work.u0, u1 = work.u1;
+        const int32_t past = work.past;
         const Span span = span_of(c, a, past, n);
-        // the first `units % pieces` parts are a unit longer
-        const int32_t len = (int32_t)((uint32_t)units / pieces), more = units - len * (int32_t)pieces;
-        const int32_t u0 = piece * len + min(piece, more), u1 = u0 + len + (piece < more ? 1 : 0);
-        const int r0 = (int)tile * ROWS, rows = min(n * a.G - r0, ROWS);
-
-        // A wave's blocks, two a step: their pages and scales 32 steps at a time, lane 2 i + e holding block e of step i.
+        // A wave's blocks, two a step, are looked up 32 steps at a time, lane 2 i + e holding block e of step i.
         const Blocks blocks(c, b, h);
         const int steps = u1 - u0;
         auto tile_of = [&](int i, int e) { return (u0 + i) * kUnit + wave * 2 + e; };
@@ -175,7 +271,7 @@ __global__ __launch_bounds__(256, 2) void kv_tree_kernel(KvView c, TreeArgs a, b
         {
             constexpr int PER = 8 / NR;                      // threads of a row
             constexpr int N = D / PER / 8;                   // 16-byte pieces of a thread
-            const int row = threadIdx.x / PER, j = threadIdx.x % PER;
+            const int row = thread / PER, j = thread % PER;
             const int r = r0 + row;
             const uint32_t flip = a.scale2 < 0.0f ? 0x80008000u : 0u;
             uint4v raw[N];
@@ -211,24 +307,27 @@ __global__ __launch_bounds__(256, 2) void kv_tree_kernel(KvView c, TreeArgs a, b
                 lds.q[(p8 >> 3) * 4 + (p8 >> 2 & 1) * 2 + (p8 & 1)][row >> 5][(p8 >> 1 & 1) * 32 + (row & 31)] = raw[i];
             }
         }
-        // the lane's rows: what they see of the cache, and of the new tokens
-        int32_t pos[NR];
-        const uint64_t* mask[NR];
+        // the lane's rows: their tokens and positions
+        auto token_of = [&](int i) { return t0 + (r0 + min(i, rows - 1)) / a.G; };       // of a row of the tile
+        auto pos_of = [&](int t) { return a.window > 0 ? min(max(a.pos[t], past), kMaxPast) : past; };
         float s2[NR];
         int32_t pos_max = past;
 #pragma unroll
-        for (int g = 0; g < NR; ++g) {
-            const int t = t0 + (r0 + min(g * 32 + col, rows - 1)) / a.G;
-            pos[g] = a.window > 0 ? min(max(a.pos[t], past), kMaxPast) : past;
-            mask[g] = a.mask + (int64_t)t * a.words;
-            pos_max = max(pos_max, pos[g]);
-        }
+        for (int g = 0; g < NR; ++g) pos_max = max(pos_max, pos_of(token_of(g * 32 + col)));
         if (a.window > 0)
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) pos_max = max(pos_max, __shfl_xor(pos_max, o));
         __syncthreads();
 #pragma unroll
         for (int g = 0; g < NR; ++g) s2[g] = fabsf(a.scale2) * lds.undo[g * 32 + col];
+
+        // 32 rows of up to 128 dimensions have room in registers
+        uint4v held[HELD ? D / 16 : 1][NR];
+        if constexpr (HELD)
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+                for (int g = 0; g < NR; ++g) held[k][g] = lds.q[k][g][lane];
 
         // blocks (of the span) that all rows see whole, but for the sinks
         const int32_t base_i = span.n_sink - span.win;
@@ -240,20 +339,17 @@ __global__ __launch_bounds__(256, 2) void kv_tree_kernel(KvView c, TreeArgs a, b
             uint4v k[ND][2];
             uint4v v[2][ND == 4 ? 2 : 1][2];
         };
-        auto fetch_k = [&](int i, int32_t pages, Raw& r) {
-            const int32_t p0 = __builtin_amdgcn_readlane(pages, (i & 31) * 2), p1 = __builtin_amdgcn_readlane(pages, (i & 31) * 2 + 1);
-            const int64_t at0 = blocks.at(p0, span.tile(tile_of(i, 0))), at1 = blocks.at(p1, span.tile(tile_of(i, 1)));
+        auto fetch_k = [&](int64_t at0, int64_t at1, Raw& r) {
             const uint8_t* p = blocks.k + (lane & 16 ? at1 : at0) + (lane & 15) * 64 + hi * 16;
 #pragma unroll
             for (int d = 0; d < ND; ++d)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) r.k[d][j] = *reinterpret_cast<const uint4v*>(p + d * 1024 + j * 32);
         };
-        auto fetch_v = [&](int i, int32_t pages, Raw& r) {
+        auto fetch_v = [&](int64_t at0, int64_t at1, Raw& r) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int32_t page = __builtin_amdgcn_readlane(pages, (i & 31) * 2 + e);
-                const uint8_t* p = blocks.v + blocks.at(page, span.tile(tile_of(i, e)));
+                const uint8_t* p = blocks.v + (e == 0 ? at0 : at1);
                 if constexpr (D == 64) {
                     // two of the four dimensions that 16 bytes hold, the lanes 16 apart the other two
 #pragma unroll
@@ -279,60 +375,81 @@ __global__ __launch_bounds__(256, 2) void kv_tree_kernel(KvView c, TreeArgs a, b
             m_run[g] = kNoMax;
             l_run[g] = 0.0f;
         }
-        // pages of the steps whose codes are fetched; of those that are computed, with their scales
-        int32_t ahead = checked(first_pages, 0), pages = ahead, pages_next = -1;
-        float ks = load_scale(blocks.ks, pages), vs = load_scale(blocks.vs, pages), ks_next = 1.0f, vs_next = 1.0f;
-        Raw raw;
-        fetch_k(0, ahead, raw);
-        fetch_v(0, ahead, raw);
-        for (int i = 0; i < steps; ++i) {
-            if (((i + 1) & 31) == 0) {
-                ahead = checked(later, i + 1);
-                later = load_pages(i + 33);
-                pages_next = ahead;
-                ks_next = load_scale(blocks.ks, ahead);
-                vs_next = load_scale(blocks.vs, ahead);
-            }
-            if (i > 0 && (i & 31) == 0) {
-                pages = pages_next;
+        // where the codes lie of the steps that are fetched; the scales, and which blocks are absent (bits), of those that
+        // are computed and of the next
+        int64_t offset;
+        float ks, vs, log_vs = 0.0f, inv_vs = 0.0f, ks_next, vs_next;
+        uint64_t absent, absent_next;
+        auto look_up = [&](int32_t page, int i0) {
+            page = checked(page, i0);
+            offset = blocks.at(page, span.tile(tile_of(i0 + (lane >> 1), lane & 1)));
+            ks_next = load_scale(blocks.ks, page);
+            vs_next = load_scale(blocks.vs, page);
+            absent_next = __ballot(page < 0);
+        };
+        look_up(first_pages, 0);
+        // one step; the codes of step i + DEPTH go into the registers that it has read
+        auto step = [&](int i, Raw& raw) {
+            const int l = (i & 31) * 2, l1 = (i + DEPTH & 31) * 2;
+            if (l == 0) {
                 ks = ks_next;
                 vs = vs_next;
+                absent = absent_next;
+                log_vs = __builtin_amdgcn_logf(vs);
+                inv_vs = __builtin_amdgcn_rcpf(vs);
             }
+            const float f[2] = {of_lane(ks, l), of_lane(ks, l + 1)};
+            const float log_scale[2] = {of_lane(log_vs, l), of_lane(log_vs, l + 1)};
+            const float inv_scale[2] = {of_lane(inv_vs, l), of_lane(inv_vs, l + 1)};
+            const uint32_t gone = (uint32_t)(absent >> l) & 3;
+            if (l1 == 0) {
+                look_up(later, i + DEPTH);
+                later = load_pages(i + DEPTH + 32);
+            }
+            const int64_t at0 = of_lane64(offset, l1), at1 = of_lane64(offset, l1 + 1);
             float16v s[NR] = {};
+            auto product = [&](int k, const uint4v (&query)[NR]) {
+                const uint4v codes = raw.k[k >> 2][k >> 1 & 1];
+                const half8 key = code_halves8<FP8>(codes[2 * (k & 1)], codes[2 * (k & 1) + 1]);
 #pragma unroll
-            for (int d = 0; d < ND; ++d)
+                for (int g = 0; g < NR; ++g)
+                    s[g] = __builtin_amdgcn_mfma_f32_32x32x16_f16(key, __builtin_bit_cast(half8, query[g]), s[g], 0, 0, 0);
+            };
+            if constexpr (HELD) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                for (int k = 0; k < D / 16; ++k) product(k, held[k]);
+            } else {
+                // the queries' operands are read kAhead products ahead; the barriers keep the reads from gathering in front,
+                // where their registers would not fit
+                constexpr int kAhead = 2;
+                uint4v queries[kAhead + 1][NR];
+                auto read_queries = [&](int k) {
 #pragma unroll
-                    for (int p = 0; p < 2; ++p) {
-                        const half8 key = code_halves8<FP8>(raw.k[d][j][2 * p], raw.k[d][j][2 * p + 1]);
+                    for (int g = 0; g < NR; ++g) queries[k % (kAhead + 1)][g] = lds.q[k][g][lane];
+                };
 #pragma unroll
-                        for (int g = 0; g < NR; ++g)
-                            s[g] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                                key, __builtin_bit_cast(half8, lds.q[(d * 2 + j) * 2 + p][g][lane]), s[g], 0, 0, 0);
-                    }
-            fetch_k(i + 1, ahead, raw);
-            const int i0 = tile_of(i, 0);
-            float f[2], log_scale[2], inv_scale[2];
-            int32_t there[2];
+                for (int k = 0; k < kAhead; ++k) read_queries(k);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int l = (i & 31) * 2 + e;
-                there[e] = __builtin_amdgcn_readlane(pages, l);
-                const float b = of_lane(vs, l);
-                f[e] = of_lane(ks, l);
-                log_scale[e] = __builtin_amdgcn_logf(b);
-                inv_scale[e] = __builtin_amdgcn_rcpf(b);
+                for (int k = 0; k < D / 16; ++k) {
+                    if (k + kAhead < D / 16) read_queries(k + kAhead);
+                    __builtin_amdgcn_sched_barrier(0);
+                    product(k, queries[k % (kAhead + 1)]);
+                }
             }
-            const bool masked = ((there[0] | there[1]) < 0) | (i0 < full_lo) | (i0 + 1 >= full_hi);
+            __builtin_amdgcn_sched_barrier(0);
+            fetch_k(at0, at1, raw);
+            const int i0 = tile_of(i, 0);
+            const bool masked = (gone != 0) | (i0 < full_lo) | (i0 + 1 >= full_hi);
             if (masked) {
+                const int own = here(col);
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int32_t tok = span.tile(i0 + e) * 16;
                     uint32_t any = 0;
 #pragma unroll
                     for (int g = 0; g < NR; ++g) {
-                        uint32_t seen = there[e] >= 0 ? tree_sight(a, mask[g], past, n, pos[g], tok) : 0u;
+                        const int t = token_of(g * 32 + own);
+                        uint32_t seen = (gone >> e & 1) == 0 ? tree_sight(a, a.mask + (int64_t)t * a.words, past, n, pos_of(t), tok) : 0u;
                         any |= seen;
                         seen >>= 4 * hi;
 #pragma unroll
@@ -417,27 +534,40 @@ __global__ __launch_bounds__(256, 2) void kv_tree_kernel(KvView c, TreeArgs a, b
 #pragma unroll
                     for (int g = 0; g < NR; ++g)
                         o[g][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value, p[g][e], o[g][i], 0, 0, 0);
+                    if (NR > 1) __builtin_amdgcn_sched_barrier(0);
                 }
-            fetch_v(i + 1, ahead, raw);
+            fetch_v(at0, at1, raw);
+        };
+        Raw raw[DEPTH];
+#pragma unroll
+        for (int k = 0; k < DEPTH; ++k) {
+            const int64_t at0 = of_lane64(offset, 2 * k), at1 = of_lane64(offset, 2 * k + 1);
+            fetch_k(at0, at1, raw[k]);
+            fetch_v(at0, at1, raw[k]);
         }
+        for (int i = 0; i < steps; i += DEPTH)
+#pragma unroll
+            for (int k = 0; k < DEPTH; ++k)
+                if (k == 0 || i + k < steps) step(i + k, raw[k]);
 
         // the four waves' sums, 64 dimensions at a time; then a thread has 2 or 4 NR of them, side by side in a row
+        const int late = here(threadIdx.x), late_col = late & 31, late_hi = late >> 5 & 1;
         float f_wave[NR];
 #pragma unroll
         for (int g = 0; g < NR; ++g) {
             l_run[g] += __shfl_xor(l_run[g], 32);
-            if (hi == 0) lds.ml[wave][g * 32 + col] = float2v{m_run[g], l_run[g]};
+            if (late_hi == 0) lds.ml[wave][g * 32 + late_col] = float2v{m_run[g], l_run[g]};
         }
         __syncthreads();
 #pragma unroll
         for (int g = 0; g < NR; ++g) {
             float m_all = kNoMax;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) m_all = fmaxf(m_all, lds.ml[w][g * 32 + col].x);
+            for (int w = 0; w < 4; ++w) m_all = fmaxf(m_all, lds.ml[w][g * 32 + late_col].x);
             f_wave[g] = __builtin_amdgcn_exp2f(m_run[g] - m_all);
         }
         constexpr int PER = 8 / NR, W = 64 / PER;            // threads of a row, and their dimensions of 64
-        const int row = threadIdx.x / PER, d0 = (threadIdx.x % PER) * W;
+        const int row = late / PER, d0 = late % PER * W;
         float m_row = kNoMax, l_row = 0.0f;
 #pragma unroll
         for (int w = 0; w < 4; ++w) m_row = fmaxf(m_row, lds.ml[w][row].x);
@@ -448,16 +578,16 @@ __global__ __launch_bounds__(256, 2) void kv_tree_kernel(KvView c, TreeArgs a, b
         for (int d = 0; d < ND; ++d) {
 #pragma unroll
             for (int g = 0; g < NR; ++g) {
-                float* to = lds.comb[wave][g * 32 + col];
+                float* to = lds.comb[wave][g * 32 + late_col];
                 if constexpr (D == 64) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        *reinterpret_cast<float2v*>(to + dim_of<D>(i, hi)) = float2v{o[g][0][i], o[g][1][i]} * f_wave[g];
+                        *reinterpret_cast<float2v*>(to + dim_of<D>(i, late_hi)) = float2v{o[g][0][i], o[g][1][i]} * f_wave[g];
                 } else {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const int k = (d & 1) * 8 + i;
-                        *reinterpret_cast<float4v*>(to + dim_of<D>(k, hi)) =
+                        *reinterpret_cast<float4v*>(to + dim_of<D>(k, late_hi)) =
                             float4v{o[g][d / 2 * 4][k], o[g][d / 2 * 4 + 1][k], o[g][d / 2 * 4 + 2][k], o[g][d / 2 * 4 + 3][k]} * f_wave[g];
                     }
                 }
@@ -472,67 +602,48 @@ __global__ __launch_bounds__(256, 2) void kv_tree_kernel(KvView c, TreeArgs a, b
             __syncthreads();
         }
 
-        bool last = true;
-        if (pieces > 1) {
-            auto put = [&](uint64_t slot) {
-                if (row >= rows) return;
-                const int64_t at = (int64_t)slot * ROWS + row;
+                    auto put = [&](int32_t slot) {
+                        if (row >= rows) return;
+                        const int64_t at = (int64_t)slot * ROWS + row;
 #pragma unroll
-                for (int d = 0; d < ND; ++d)
+                        for (int d = 0; d < ND; ++d)
 #pragma unroll
-                    for (int j = 0; j < W / 4; ++j) {
-                        float* to = a.part_o + at * D + d * 64 + d0 + j * 4;
-                        put_shared(to, float2v{sums[d][j].x, sums[d][j].y});
-                        put_shared(to + 2, float2v{sums[d][j].z, sums[d][j].w});
-                    }
-                if (d0 == 0) put_shared((float*)&a.part_ml[at], float2v{m_row, l_row});
-            };
-            // adds n parts, `step` apart from `first`, in their order
-            auto add = [&](uint64_t first, int step, int n) {
-                if (row >= rows) return;
-                m_row = kNoMax;
-                l_row = 0.0f;
+                            for (int j = 0; j < W / 4; ++j) {
+                                float* to = a.part_o + at * D + d * 64 + d0 + j * 4;
+                                put_shared(to, float2v{sums[d][j].x, sums[d][j].y});
+                                put_shared(to + 2, float2v{sums[d][j].z, sums[d][j].w});
+                            }
+                        if (d0 == 0) put_shared((float*)&a.part_ml[at], float2v{m_row, l_row});
+                    };
+                                        auto add = [&](auto slot, int from, int step, int n) {
+                        if (row >= rows) return;
+                        m_row = kNoMax;
+                        l_row = 0.0f;
 #pragma unroll
-                for (int d = 0; d < ND; ++d)
+                        for (int d = 0; d < ND; ++d)
 #pragma unroll
-                    for (int j = 0; j < W / 4; ++j) sums[d][j] = float4v{0, 0, 0, 0};
-                for (int i = 0; i < n; ++i) {
-                    const int64_t at = (int64_t)(first + (uint64_t)i * step) * ROWS + row;
-                    const float2v ml = get_shared((const float*)&a.part_ml[at]);
-                    float2v x[ND][W / 4][2];
+                            for (int j = 0; j < W / 4; ++j) sums[d][j] = float4v{0, 0, 0, 0};
+                        for (int i = 0; i < n; ++i) {
+                            const int64_t at = (int64_t)slot(from + i * step) * ROWS + row;
+                            const float2v ml = get_shared((const float*)&a.part_ml[at]);
+                            float2v x[ND][W / 4][2];
 #pragma unroll
-                    for (int d = 0; d < ND; ++d)
+                            for (int d = 0; d < ND; ++d)
 #pragma unroll
-                        for (int j = 0; j < W / 4; ++j)
+                                for (int j = 0; j < W / 4; ++j)
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) x[d][j][e] = get_shared(a.part_o + at * D + d * 64 + d0 + j * 4 + 2 * e);
-                    const float top = fmaxf(m_row, ml.x), by = __builtin_amdgcn_exp2f(m_row - top), f = __builtin_amdgcn_exp2f(ml.x - top);
-                    m_row = top;
-                    l_row = l_row * by + ml.y * f;
+                                    for (int e = 0; e < 2; ++e) x[d][j][e] = get_shared(a.part_o + at * D + d * 64 + d0 + j * 4 + 2 * e);
+                            const float top = fmaxf(m_row, ml.x), by = __builtin_amdgcn_exp2f(m_row - top), f = __builtin_amdgcn_exp2f(ml.x - top);
+                            m_row = top;
+                            l_row = l_row * by + ml.y * f;
 #pragma unroll
-                    for (int d = 0; d < ND; ++d)
+                            for (int d = 0; d < ND; ++d)
 #pragma unroll
-                        for (int j = 0; j < W / 4; ++j)
-                            sums[d][j] = sums[d][j] * by + float4v{x[d][j][0].x, x[d][j][0].y, x[d][j][1].x, x[d][j][1].y} * f;
-                }
-            };
-            // Parts are added in groups of kJoin: whoever finishes a group's last part adds the group's parts, whoever
-            // finishes the last group adds the groups' sums; always in the order of the parts.
-            const int gr = piece / kJoin, members = min(kJoin, (int)pieces - gr * kJoin), groups = ((int)pieces - 1) / kJoin + 1;
-            const uint64_t lead = seg + (uint32_t)gr * kJoin;        // the group's first part
-            put(seg + (uint32_t)piece);
-            last = arrive(a.arrived + lead * 2, members);
-            if (last) {
-                add(lead, 1, members);
-                if (groups > 1) {
-                    // the group's sum in the place of its first part, which all of the workgroup has read
-                    __syncthreads();
-                    put(lead);
-                    last = arrive(a.arrived + seg * 2 + 1, groups);
-                    if (last) add(seg, kJoin, groups);
-                }
-            }
-        }
+                                for (int j = 0; j < W / 4; ++j)
+                                    sums[d][j] = sums[d][j] * by + float4v{x[d][j][0].x, x[d][j][0].y, x[d][j][1].x, x[d][j][1].y} * f;
+                        }
+                    };
+        const bool last = work.join(put, add);
         if (last && row < rows) {
             const float norm = l_row > 0.0f ? 1.0f / l_row : 0.0f;
             const int r = r0 + row;
@@ -566,35 +677,41 @@ hipError_t launch_kv_tree(const KvView& c, const KvTree& t, const void* q, int64
     a.mask = t.mask;
     a.words = t.words;
     a.pos = t.pos;
-    // tiles of 32 rows where no tree has more, or where the sums of 64 would not fit the registers
-    const int rows = c.D == 256 || (int64_t)c.max_new * a.G <= 32 ? 32 : 64;
+    // Tiles of 64 rows halve the conversions and the codes' way from the caches, but leave half as many workgroups something
+    // to do and less room for codes on their way.  Measured with 32 and 64, 8 kv heads of 128, us: 32 sequences of 2,000
+    // tokens with 48 rows 33 and 62, 96 rows 57 and 50, 256 rows 115 and 94; 4 of 16,000 with 128 rows 61 and 104, 512 rows
+    // 159 and 171; 2 of 88,000 with 512 rows 530 and 455.
+    const int64_t all_rows = (int64_t)c.T * a.G, most_rows = (int64_t)c.max_new * a.G;
+    const bool wide = c.D != 256 && ((most_rows > 64 && all_rows >= 3072) || (most_rows >= 256 && all_rows * c.limit >= 1 << 26));
+    const int rows = wide ? 64 : 32;
+    const int64_t tiles = (int64_t)c.T * a.G / rows + c.B;
+    const int64_t line = ((int64_t)c.limit / (16 * kUnit) + 2 + kTreeStart) * c.H;
+    if (tiles * c.H >= (int64_t)1 << 24 || line >= (int64_t)1 << 31) return hipErrorInvalidConfiguration;
+    // workgroups that fit the device, as far as the workspace has two slots for each
     WsCarve ws{(char*)workspace, (size_t)workspace_bytes};
     a.arrived = ws.take<uint32_t>(kMaxParts * 2);
-    // as many parts as workgroups fit the device, and 2.5 for each segment where that is more; segments stay whole
-    // where the workspace does not hold that many parts
-    const int64_t segments = ((int64_t)c.T * a.G / rows + c.B) * c.H, fit = (int64_t)n_cu * 2;
-    if (segments >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
-    const int64_t room = std::min<int64_t>((workspace_bytes - (int64_t)ws.off - 1024) / (rows * (c.D + 2) * 4), kMaxParts);
-    const bool cut = segments * 3 <= room * 2;
-    const int64_t wgs = cut ? std::min(std::max(fit, segments * 5 / 2), room) : std::min<int64_t>(segments, 1 << 20);
-    if (cut) {
-        a.part_ml = ws.take<float2v>(wgs * rows);
-        a.part_o = ws.take<float>(wgs * rows * c.D);
-    }
+    const int64_t room = (workspace_bytes - (int64_t)ws.off - 512) / ((int64_t)rows * (c.D + 2) * 4 * 2);
+    a.fit = (int32_t)std::min<int64_t>({(int64_t)n_cu * 2, room, kMaxParts / 2});
+    a.part_ml = ws.take<float2v>((int64_t)a.fit * 2 * rows);
+    a.part_o = ws.take<float>((int64_t)a.fit * 2 * rows * c.D);
     if (!ws.ok()) return hipErrorInvalidConfiguration;
-    auto run = [&](auto d, auto fp8, auto nr) {
-        kv_tree_kernel<decltype(d)::value, decltype(fp8)::value, decltype(nr)::value><<<(uint32_t)wgs, 256, 0, s>>>(c, a, cut);
+    a.groups = tiles + a.fit;
+    const int64_t wgs = std::min<int64_t>(a.groups, 1 << 20);
+    auto run = [&](auto d, auto fp8) {
+        constexpr int D = decltype(d)::value;
+        constexpr bool FP8 = decltype(fp8)::value;
+        if constexpr (D != 256)
+            if (rows == 64) {
+                kv_tree_kernel<D, FP8, 2><<<(uint32_t)wgs, 256, 0, s>>>(c, a);
+                return hipGetLastError();
+            }
+        kv_tree_kernel<D, FP8, 1><<<(uint32_t)wgs, 256, 0, s>>>(c, a);
         return hipGetLastError();
     };
-    auto by_rows = [&](auto d, auto fp8) {
-        if constexpr (decltype(d)::value != 256)
-            if (rows == 64) return run(d, fp8, std::integral_constant<int, 2>{});
-        return run(d, fp8, std::integral_constant<int, 1>{});
-    };
     auto by_dim = [&](auto fp8) {
-        if (c.D == 64) return by_rows(std::integral_constant<int, 64>{}, fp8);
-        if (c.D == 128) return by_rows(std::integral_constant<int, 128>{}, fp8);
-        return by_rows(std::integral_constant<int, 256>{}, fp8);
+        if (c.D == 64) return run(std::integral_constant<int, 64>{}, fp8);
+        if (c.D == 128) return run(std::integral_constant<int, 128>{}, fp8);
+        return run(std::integral_constant<int, 256>{}, fp8);
     };
     return c.fp8 ? by_dim(std::true_type{}) : by_dim(std::false_type{});
 }

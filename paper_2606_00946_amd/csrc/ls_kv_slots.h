@@ -44,16 +44,54 @@ constexpr TileRows tile_rows(int64_t i, int32_t n, int32_t G, int32_t tile) {
     return {r0, (int32_t)least(left, tile)};
 }
 
-// A tree's parts, `pairs` of (head, piece) for each of `tiles` row tiles: eight pairs beside
-// each other, then their next tile, so that the tiles that read the same codes run on one
-// XCD (workgroups go round eight) at about one time.
-struct TreePlace {
-    uint32_t pair, tile;
+// Attention of trees.  A sequence's heads lie one behind the other on a line, each with
+// kTreeStart units for the start and the end and then its own; the line is cut into equal
+// stretches, at the same places for all of the sequence's row tiles, and a workgroup has one
+// stretch of one tile.  A head that several of them share falls into pieces; one of fewer than
+// kTreeLeast units goes to the neighbour instead.
+constexpr int32_t kTreeStart = 6, kTreeLeast = 4;
+
+// The length of a line's stretches, at most `want` of them: whole heads, or equal parts of
+// each, where cuts anywhere would gain less than the start and the end that a cut head costs
+// once more; not so short that pieces vanish.
+constexpr int32_t tree_stretch(int32_t units, int32_t heads, int32_t want) {
+    const int32_t head = units + kTreeStart, each = want < heads ? (heads + want - 1) / want : 1, of_head = want < heads ? 1 : want / heads;
+    const int32_t even = each * ((head + of_head - 1) / of_head), any = (head * heads + want - 1) / want;
+    const int32_t least = kTreeStart + 2 * kTreeLeast, best = even <= any + kTreeStart * 3 / 2 ? even : any;
+    return best >= least || best == each * head ? best : head < least ? head : least;
+}
+
+// A head's unit at which a cut lies, x behind the head's place on the line.
+constexpr int32_t tree_cut(int32_t x, int32_t units) {
+    const int32_t u = x - kTreeStart;
+    return u < kTreeLeast ? 0 : u > units - kTreeLeast ? units : u;
+}
+
+// The stretches (`per` long) with pieces of the head at `at`: first and last.
+struct TreePieces {
+    int32_t first, last;
 };
-constexpr TreePlace tree_place(uint32_t at, uint32_t pairs, uint32_t tiles) {
-    const uint32_t even = pairs & ~7u;
+constexpr TreePieces tree_pieces(int32_t at, int32_t units, int32_t per) {
+    TreePieces p = {at / per, (at + kTreeStart + units - 1) / per};
+    if (p.first < p.last && tree_cut((p.first + 1) * per - at, units) == 0) ++p.first;
+    if (p.first < p.last && tree_cut(p.last * per - at, units) == units) --p.last;
+    return p;
+}
+
+// Where the sums of a head's j-th piece lie: a stretch has at most one piece that starts
+// inside a head, and at most one that is cut off at its end.
+constexpr int32_t tree_slot(int32_t first, int32_t j) { return j == 0 ? 2 * first + 1 : 2 * (first + j); }
+
+// Stretch and tile of a sequence's `at`-th workgroup: eight stretches beside each other, then
+// their next tile, so that the tiles that read the same codes run on one XCD (workgroups go
+// round eight) at about one time.
+struct TreePlace {
+    int32_t stretch, tile;
+};
+constexpr TreePlace tree_place(int32_t at, int32_t stretches, int32_t tiles) {
+    const int32_t even = stretches & ~7;
     if (at < even * tiles) return {at / (8 * tiles) * 8 + (at & 7), at % (8 * tiles) >> 3};
-    const uint32_t r = at - even * tiles, w = pairs - even;
+    const int32_t r = at - even * tiles, w = stretches - even;
     return {even + r % w, r / w};
 }
 

@@ -96,7 +96,7 @@ def code_of(x, fmt):
 
 def keep(cache, new_off, past, pages, kept, n_kept):
     """Changes `cache` (a kv_oracle.Cache) as ls_kv_keep does.  Products and quotients are rounded to 32 bits as the
-    definition's scale and codes need it: old / new scale as old * (1 / new)."""
+    definition's scale and codes need it: a / 127 as a * (1 / 127), old / new scale as old * (1 / new)."""
     f32 = np.float32
     for name in "kv":
         at = ko.offsets(cache.page, cache.D, name == "v")
@@ -128,7 +128,7 @@ def keep(cache, new_off, past, pages, kept, n_kept):
                         top = np.abs(ko.code_values(old_codes[pf][:, at[rf]], cache.fmt)).max(1)
                         a = (top.astype(f32) * old_scale[pf].astype(f32)).astype(np.float64)
                         want = ko.scale_of(a, cache.fmt)
-                        new = np.maximum(new, (a.astype(f32) / f32(127)).clip(f32(ko.SCALE_MIN), f32(ko.SCALE_MAX))
+                        new = np.maximum(new, (a.astype(f32) * (f32(1) / f32(127))).clip(f32(ko.SCALE_MIN), f32(ko.SCALE_MAX))
                                          if cache.fmt == "int8" else want)
                 if not moved:
                     continue

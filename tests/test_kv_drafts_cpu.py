@@ -19,13 +19,32 @@ PROGRAM = r"""
 #include <cstdlib>
 #include "ls_kv_slots.h"
 
-// argv: 'p' pairs tiles: pair and tile of each part; or 'b', then any number of (rel, n, gone, sink, lo, hi): the bits
+// argv: 'l' units, heads, wanted stretches: the pieces of every stretch (stretch, head, units, first and last stretch of the
+// head, slot); 'p' stretches tiles: stretch and tile of each workgroup; 'b', then any number of (rel, n, gone, sink, lo,
+// hi): the bits
 int main(int argc, char** a) {
+    if (a[1][0] == 'l') {
+        const int units = atoi(a[2]), heads = atoi(a[3]);
+        const long long part = units + ls::kTreeStart, line = part * heads, per = ls::tree_stretch(units, heads, atoi(a[4]));
+        const long long w = (line + per - 1) / per;
+        for (long long s = 0; s < w; ++s) {
+            const long long lo = s * per, hi = lo + per < line ? lo + per : line;
+            for (long long h = lo / part; h * part < hi; ++h) {
+                const long long place = h * part;
+                const int u0 = ls::tree_cut(lo - place, units), u1 = place + part <= hi ? units : ls::tree_cut(hi - place, units);
+                if (u0 >= u1) continue;
+                const ls::TreePieces p = ls::tree_pieces(place, units, per);
+                const long long slot = u0 > 0 || u1 < units ? (long long)ls::tree_slot(p.first, (int)(s - p.first)) : -1;
+                printf("%lld %lld %d %d %lld %lld %lld\n", s, h, u0, u1, (long long)p.first, (long long)p.last, slot);
+            }
+        }
+        return 0;
+    }
     if (a[1][0] == 'p') {
-        const uint32_t pairs = atoi(a[2]), tiles = atoi(a[3]);
-        for (uint32_t i = 0; i < pairs * tiles; ++i) {
-            const ls::TreePlace p = ls::tree_place(i, pairs, tiles);
-            printf("%u %u\n", p.pair, p.tile);
+        const int w = atoi(a[2]), tiles = atoi(a[3]);
+        for (int i = 0; i < w * tiles; ++i) {
+            const ls::TreePlace p = ls::tree_place(i, w, tiles);
+            printf("%d %d\n", p.stretch, p.tile);
         }
         return 0;
     }
@@ -47,15 +66,42 @@ def program(tmp_path_factory):
     return lambda *args: subprocess.check_output([exe, *map(str, args)], text=True).split()
 
 
-@pytest.mark.parametrize("pairs", [1, 3, 7, 8, 9, 16, 61])
+@pytest.mark.parametrize("heads", [1, 2, 3, 8])
+@pytest.mark.parametrize("units", [1, 2, 7, 8, 9, 14, 40, 333, 5000])
+def test_every_unit_is_dealt_once(program, units, heads):
+    """A head's pieces follow each other over its units, a stretch each, in slots of their own; none is tiny."""
+    for want in (1, 2, 3, 5, 7, 8, 9, 16, 31, 64, 200, 512):
+        got = np.array(program("l", units, heads, want), int).reshape(-1, 7)
+        assert got[:, 0].max() < want
+        slots = got[got[:, 6] >= 0, 6]
+        assert len(set(slots)) == len(slots) and (slots < 2 * want).all()
+        assert set(got[:, 1]) == set(range(heads))
+        for h in range(heads):
+            mine = got[got[:, 1] == h]
+            assert mine[0, 2] == 0 and mine[-1, 3] == units and (mine[1:, 2] == mine[:-1, 3]).all()
+            assert (np.diff(mine[:, 0]) == 1).all()
+            if len(mine) > 1:
+                assert (mine[:, 4] == mine[0, 0]).all() and (mine[:, 5] == mine[-1, 0]).all()
+                assert (mine[:, 3] - mine[:, 2]).min() >= 4 and (mine[:, 6] >= 0).all()
+            else:
+                assert mine[0, 6] == -1
+
+
+@pytest.mark.parametrize("units,want,each", [(3, 512, 1), (16, 8, 1), (16, 5, 2), (16, 4, 2), (16, 3, 3), (16, 1, 8)])
+def test_short_heads_stay_whole(program, units, want, each):
+    got = np.array(program("l", units, 8, want), int).reshape(-1, 7)
+    assert got[:, :2].tolist() == [[i // each, i] for i in range(8)]
+
+
+@pytest.mark.parametrize("stretches", [1, 3, 7, 8, 9, 16, 61])
 @pytest.mark.parametrize("tiles", [1, 2, 3, 17])
-def test_parts_are_dealt_once(program, pairs, tiles):
-    got = np.array(program("p", pairs, tiles), int).reshape(-1, 2)
-    assert sorted(map(tuple, got)) == [(p, t) for p in range(pairs) for t in range(tiles)]
-    # a full group's tiles of one pair lie eight parts apart
+def test_every_stretch_and_tile_has_a_workgroup(program, stretches, tiles):
+    got = np.array(program("p", stretches, tiles), int).reshape(-1, 2)
+    assert sorted(map(tuple, got)) == [(s, t) for s in range(stretches) for t in range(tiles)]
+    # of a full group, the tiles of one stretch lie eight workgroups apart
     at = {tuple(x): i for i, x in enumerate(got)}
-    for p in range(pairs & ~7):
-        assert [at[p, t] - at[p, 0] for t in range(tiles)] == [8 * t for t in range(tiles)]
+    for s in range(stretches & ~7):
+        assert [at[s, t] - at[s, 0] for t in range(tiles)] == [8 * t for t in range(tiles)]
 
 
 def test_bits_follow_the_definition(program):
