@@ -292,6 +292,18 @@ def test_pools_of_many_chunks(ctx, n_pages, share):
     check_compact(ctx, lay, table, in_place=True)
 
 
+@pytest.mark.parametrize("n_pages,rows,width,share", [
+    (65535, 3, 20000, 0.6), (65536, 1, 65536, 0.5), (65537, 7, 9000, 0.5), (70001, 2, 10, 0.9),    # either side of one workgroup's plan
+    (5000, 2, 65536, 0.4), (5000, 1, 131073, 0.4), (12289, 64, 2049, 0.97)])                       # and of its table
+def test_large_pools_and_tables(ctx, n_pages, rows, width, share):
+    lay = Layers(n_pages, layers=1, H=1, D=64, seed=n_pages)
+    ids = np.where(lay.rng.rand(n_pages) < share)[0]
+    table = lay.rng.choice(ids, (rows, width))
+    table[lay.rng.rand(rows, width) < 0.1] = -1
+    note(f"kv compact {n_pages} pages, table {rows} x {width}")
+    check_compact(ctx, lay, table)
+
+
 def test_nothing_and_all_named(ctx):
     note("kv compact nothing, all, above, below")
     check_compact(ctx, Layers(20, seed=1), np.full((2, 3), -1))
