@@ -16,14 +16,17 @@ namespace {
 // A sequence's kept tokens: the list ends before the first entry that is not above
 // the one before it, or not one of the new tokens.  Kept token i comes from new
 // token kept[i] >= i, so a page's tokens come from it or from later pages, and
-// pages may be rewritten in their order.
-__device__ __forceinline__ int kept_count(const int32_t* kept, int want, int n) {
+// pages may be rewritten in their order.  `moves`: the first that is not in its place,
+// and none after it is.
+__device__ __forceinline__ int kept_count(const int32_t* kept, int want, int n, int& moves) {
     const int lane = threadIdx.x & 63;
     want = min(max(want, 0), n);
+    moves = want;
     for (int i0 = 0; i0 < want; i0 += 64) {
         const int i = i0 + lane;
         const int32_t k = i < want ? kept[i] : n, before = i > 0 && i < want ? kept[i - 1] : -1;
-        const uint64_t bad = __ballot(k <= before || k >= n);
+        const uint64_t bad = __ballot(k <= before || k >= n), away = __ballot(k != i);
+        if (away) moves = min(moves, i0 + __ffsll((long long)away) - 1);
         if (bad) return min(i0 + __ffsll((long long)bad) - 1, want);
     }
     return want;
@@ -58,20 +61,20 @@ __device__ __forceinline__ float kept_scale(float a) {
     return FP8 ? scale_of<true>(a) : fminf(fmaxf(a * (1.0f / 127.0f), kScaleMin), kScaleMax);
 }
 
-// A wave: one layer's keys or values of a sequence and head.  Page by page, 16 tokens
+// A wave: one layer's keys or values of a sequence and head, kept tokens i0 to n.  Page by page, 16 tokens
 // at a time: a lane holds, of every 64 dimensions, 16 of one key, or four of each of four
 // values.  Once for the largest magnitude that moves in, once for the codes; a page of
 // 16 tokens stays in registers between the two.
 template <int D, bool FP8, bool VALUE>
 __device__ __forceinline__ void keep_rows(const KvView& c, uint8_t* codes, float* scales, int b, int h, int64_t past,
-                                          const int32_t* kept, int n) {
+                                          const int32_t* kept, int i0, int n) {
     constexpr int ND = D / 64, NT = VALUE ? 4 : 1;       // tokens of a lane
     const int lane = threadIdx.x & 63;
     const int first = VALUE ? (lane >> 4) * 4 : lane >> 2;      // the lane's first token of a block
     const int64_t head = (int64_t)c.page * D;
-    for (int64_t j = past >> c.page_shift; j << c.page_shift < past + n; ++j) {
+    for (int64_t j = (past + i0) >> c.page_shift; j << c.page_shift < past + n; ++j) {
         const int64_t pos0 = j << c.page_shift;
-        const int r0 = (int)max(past - pos0, (int64_t)0), r1 = (int)min(past + n - pos0, (int64_t)c.page);
+        const int r0 = (int)max(past + i0 - pos0, (int64_t)0), r1 = (int)min(past + n - pos0, (int64_t)c.page);
         const int64_t page = j < c.W ? page_id(c, b, (int)j) : -1;
         if (page < 0) continue;
         uint8_t* mine = codes + (page * c.H + h) * head;
@@ -177,12 +180,13 @@ __global__ __launch_bounds__(256) void kv_keep_kernel(KvView c, KvLayers l, cons
     int t0, n;
     seq_rows(c, b, t0, n);
     const int64_t past = min(max(c.past[b], 0), 1 << 30);
-    n = kept_count(kept + t0, n_kept[b], n);
-    if (n == 0) return;
+    int i0;
+    n = kept_count(kept + t0, n_kept[b], n, i0);
+    if (i0 >= n) return;
     if (value)
-        keep_rows<D, FP8, true>(c, l.codes[1][layer], l.scales[1][layer], b, h, past, kept + t0, n);
+        keep_rows<D, FP8, true>(c, l.codes[1][layer], l.scales[1][layer], b, h, past, kept + t0, i0, n);
     else
-        keep_rows<D, FP8, false>(c, l.codes[0][layer], l.scales[0][layer], b, h, past, kept + t0, n);
+        keep_rows<D, FP8, false>(c, l.codes[0][layer], l.scales[0][layer], b, h, past, kept + t0, i0, n);
 }
 
 // ---- forking ----------------------------------------------------------------------
