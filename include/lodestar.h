@@ -608,7 +608,7 @@ int ls_kv_read(ls_ctx* ctx, const ls_kv_cache* cache, const ls_kv_batch* batch, 
  * own ancestors, and keeps one path.  ls_kv_append_at and ls_kv_attention_tree
  * work on one layer's cache like the calls above, the others on all layers'
  * caches in one call: `caches` is a host array of n_caches of them, all with the
- * same dtype, n_kv_heads, head_dim, page_tokens and n_pages.
+ * same dtype, n_kv_heads, head_dim, page_tokens and n_pages, and none twice.
  *
  * ls_positions  positions of the call's rows for the rotation (host struct):
  *   n_axes       1..LS_MAX_AXES
@@ -636,7 +636,9 @@ int ls_kv_read(ls_ctx* ctx, const ls_kv_cache* cache, const ls_kv_batch* batch, 
  *   entry that does not, or is no new token of the sequence.  A token whose old or new page is absent
  *   stays where it is.  A page that tokens move into gets the larger of its scale and the one that the largest
  *   magnitude among them asks for (ls_kv_append's rule, the division by 127 as a product with 1 / 127 in fp32), and
- *   what it holds up to the last kept token is brought to it; codes are rounded once more where the scales differ.  What lies behind the last kept token is nobody's.
+ *   what it holds up to the last kept token is brought to it; codes are rounded once more where the scales differ.
+ *   What lies behind the last kept token is nobody's.  As with ls_kv_append, no two sequences of a call may share a
+ *   page from past[b] on.
  * ls_kv_fork  for i < n_forks, row dst[i] of pages_out takes over the first tokens[i] tokens of row src[i] of
  *   pages (tables int32 [n_rows x pages_stride]; src, dst, tokens int32 [n_forks], all on the device): entries of
  *   pages that these tokens fill are copied, so both rows share them; where the last page is only partly filled, its

@@ -7,10 +7,19 @@
 //
 // A tree's rows (new tokens x query heads of one kv head) are more than a decode step's
 // and fewer than a prompt's, over as many cached tokens: at 4 D operations and 2 D
-// bytes a token, reading and computing take the same time at about 130 rows.
+// bytes a token, reading (5.1 TB/s) and computing (1,170 TFLOP/s) take the same time at
+// about 115 rows.
 // So the tokens are what is dealt out: a wave takes 32 of a unit's 128 tokens with all
 // of a tile's 32 or 64 rows, codes go from memory to registers in 16-byte loads and
 // each operand made of them serves all rows; only the queries are in LDS.
+//
+// Measured, 8 kv heads: 32 sequences of 16 to 64 drafts x 4 heads of 128 over 64 to 8,192 tokens
+// (fp8) 98 us, 393 TFLOP/s; 2 of 64 x 8 over 64k to 128k tokens (int8) 462 us, 780 TFLOP/s; 24 of
+// 33 to 160 x 2 heads of 64 under a window of 2,048 (int8) 81 us; one of 8 drafts over 300
+// tokens 11.7 us.  In the long one the matrix pipes are busy for 40 % of the cycles and the vector
+// instructions (the exponential, its argument and sum, conversions of codes and weights) take 61 %: a wave
+// alternates between the two, and two waves a SIMD, which is what the registers allow, seldom
+// have one in each.  Raising a wave's priority for its products did not change that.
 #include <algorithm>
 
 #include "k_kv_attend.h"
@@ -172,6 +181,8 @@ struct TreeWork {
             if (found) return false;
             if (pass == 0) {
                 tiles = (float)groups;
+                // offsets that overlap make more tiles than the launch has workgroups for: a cut head might be left half done
+                if (groups > a.groups - a.fit) pass = kTries + 1;
             } else if ((pass <= kTries ? groups : cut) <= a.fit) {
                 found = true;
                 continue;
@@ -602,47 +613,47 @@ __global__ __launch_bounds__(256, 2) void kv_tree_kernel(KvView c, TreeArgs a) {
             __syncthreads();
         }
 
-                    auto put = [&](int32_t slot) {
-                        if (row >= rows) return;
-                        const int64_t at = (int64_t)slot * ROWS + row;
+        auto put = [&](int32_t slot) {
+            if (row >= rows) return;
+            const int64_t at = (int64_t)slot * ROWS + row;
 #pragma unroll
-                        for (int d = 0; d < ND; ++d)
+            for (int d = 0; d < ND; ++d)
 #pragma unroll
-                            for (int j = 0; j < W / 4; ++j) {
-                                float* to = a.part_o + at * D + d * 64 + d0 + j * 4;
-                                put_shared(to, float2v{sums[d][j].x, sums[d][j].y});
-                                put_shared(to + 2, float2v{sums[d][j].z, sums[d][j].w});
-                            }
-                        if (d0 == 0) put_shared((float*)&a.part_ml[at], float2v{m_row, l_row});
-                    };
-                                        auto add = [&](auto slot, int from, int step, int n) {
-                        if (row >= rows) return;
-                        m_row = kNoMax;
-                        l_row = 0.0f;
+                for (int j = 0; j < W / 4; ++j) {
+                    float* to = a.part_o + at * D + d * 64 + d0 + j * 4;
+                    put_shared(to, float2v{sums[d][j].x, sums[d][j].y});
+                    put_shared(to + 2, float2v{sums[d][j].z, sums[d][j].w});
+                }
+            if (d0 == 0) put_shared((float*)&a.part_ml[at], float2v{m_row, l_row});
+        };
+        auto add = [&](auto slot, int from, int step, int n) {
+            if (row >= rows) return;
+            m_row = kNoMax;
+            l_row = 0.0f;
 #pragma unroll
-                        for (int d = 0; d < ND; ++d)
+            for (int d = 0; d < ND; ++d)
 #pragma unroll
-                            for (int j = 0; j < W / 4; ++j) sums[d][j] = float4v{0, 0, 0, 0};
-                        for (int i = 0; i < n; ++i) {
-                            const int64_t at = (int64_t)slot(from + i * step) * ROWS + row;
-                            const float2v ml = get_shared((const float*)&a.part_ml[at]);
-                            float2v x[ND][W / 4][2];
+                for (int j = 0; j < W / 4; ++j) sums[d][j] = float4v{0, 0, 0, 0};
+            for (int i = 0; i < n; ++i) {
+                const int64_t at = (int64_t)slot(from + i * step) * ROWS + row;
+                const float2v ml = get_shared((const float*)&a.part_ml[at]);
+                float2v x[ND][W / 4][2];
 #pragma unroll
-                            for (int d = 0; d < ND; ++d)
+                for (int d = 0; d < ND; ++d)
 #pragma unroll
-                                for (int j = 0; j < W / 4; ++j)
+                    for (int j = 0; j < W / 4; ++j)
 #pragma unroll
-                                    for (int e = 0; e < 2; ++e) x[d][j][e] = get_shared(a.part_o + at * D + d * 64 + d0 + j * 4 + 2 * e);
-                            const float top = fmaxf(m_row, ml.x), by = __builtin_amdgcn_exp2f(m_row - top), f = __builtin_amdgcn_exp2f(ml.x - top);
-                            m_row = top;
-                            l_row = l_row * by + ml.y * f;
+                        for (int e = 0; e < 2; ++e) x[d][j][e] = get_shared(a.part_o + at * D + d * 64 + d0 + j * 4 + 2 * e);
+                const float top = fmaxf(m_row, ml.x), by = __builtin_amdgcn_exp2f(m_row - top), f = __builtin_amdgcn_exp2f(ml.x - top);
+                m_row = top;
+                l_row = l_row * by + ml.y * f;
 #pragma unroll
-                            for (int d = 0; d < ND; ++d)
+                for (int d = 0; d < ND; ++d)
 #pragma unroll
-                                for (int j = 0; j < W / 4; ++j)
-                                    sums[d][j] = sums[d][j] * by + float4v{x[d][j][0].x, x[d][j][0].y, x[d][j][1].x, x[d][j][1].y} * f;
-                        }
-                    };
+                    for (int j = 0; j < W / 4; ++j)
+                        sums[d][j] = sums[d][j] * by + float4v{x[d][j][0].x, x[d][j][0].y, x[d][j][1].x, x[d][j][1].y} * f;
+            }
+        };
         const bool last = work.join(put, add);
         if (last && row < rows) {
             const float norm = l_row > 0.0f ? 1.0f / l_row : 0.0f;

@@ -1445,6 +1445,9 @@ int kv_layers(ls_ctx* c, const ls_kv_cache* caches, int32_t n, ls::KvView* v) {
         if (a.dtype != b.dtype || a.n_kv_heads != b.n_kv_heads || a.head_dim != b.head_dim ||
             a.page_tokens != b.page_tokens || a.n_pages != b.n_pages)
             return fail(c, LS_ERR_INVALID, "the caches must have the same dtype, heads, dimensions, page tokens and pages");
+        // a cache that is given twice would be rewritten by two waves at once
+        for (int32_t j = 0; j < i; ++j)
+            if (caches[j].k == b.k || caches[j].v == b.v) return fail(c, LS_ERR_INVALID, "a cache is given twice");
     }
     return LS_OK;
 }

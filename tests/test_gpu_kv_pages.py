@@ -490,6 +490,10 @@ def test_refusals(ctx):
             bad = (lodestar.ls_kv_cache * 2).from_buffer_copy(lay.caches.c)
             setattr(bad[1], field, value)
             refused(word, call(c=bad))
+        for name in "kv":
+            bad = (lodestar.ls_kv_cache * 2).from_buffer_copy(lay.caches.c)
+            setattr(bad[1], name, getattr(bad[0], name))
+            refused("twice", call(c=bad))
     refused("batch must", keep(b=None))
     refused("kept", keep(k=None))
     refused("n_kept", keep(m=None))

@@ -280,6 +280,37 @@ def test_padded_batches(ctx):
     torch.cuda.synchronize()
 
 
+def test_overlapping_sequences_leave_nothing_behind(ctx):
+    """Offsets that overlap name far more rows than the call has: what a launch has no workgroups for must not stay half done
+    in the workspace."""
+    import torch
+    s = grown(Setup([(20000, 64)], H=1, D=64, seed=13))
+    q, past = s.tensor(4), s.batch.past.clone()
+    out = torch.empty_like(q)
+
+    def lengths():
+        outs = []
+        for k in range(40, 157, 2):
+            s.batch.past.fill_(128 * k)
+            ctx.ls_kv_attention_tree(s.cache, s.batch, s.tree, q, out)
+            outs.append(out.clone())
+        return torch.stack(outs)
+
+    note("kv tree before overlapping offsets")
+    before = lengths()
+    for pairs in (70, 80, 81, 82, 83, 84, 85, 90):
+        off = torch.tensor([0, s.T] * pairs + [0, 0, s.T], dtype=torch.int32, device="cuda")
+        long = torch.zeros(len(off) - 1, dtype=torch.int32, device="cuda")
+        long[-1] = 20000
+        batch = lodestar.KVBatch(off, long, s.batch.pages.repeat(len(long), 1), s.T, s.T)
+        note(f"kv tree {pairs} overlapping sequences")
+        ctx.ls_kv_attention_tree(s.cache, batch, s.tree, q, out)
+        torch.cuda.synchronize()
+    assert torch.equal(before, lengths())
+    s.batch.past.copy_(past)
+    check(ctx, s, 4, q=q)
+
+
 def test_offsets_past_32_bits(ctx):
     """Pages beyond 4 GiB of the pool."""
     import torch
