@@ -168,7 +168,12 @@ __device__ __forceinline__ void keep_rows(const KvView& c, uint8_t* codes, float
     }
 }
 
-// Waves: (layer, sequence, head, key or value).
+// Waves: (layer, sequence, head, key or value).  Measured: 64 sequences of 16 to 64 drafts, up to 9
+// of them kept, 32 layers of 8 heads of 128 (int8): 52 us, where its bytes would take 4.  Vector
+// instructions take 62 % of the cycles (540 a wave, most of them for the 16 tokens of a block whichever
+// of them move), the chain list, table, codes the rest.  Waves that keep 2, 4 or 8 heads
+// in turn read lists and tables less often and decode only what moves, but wait for one head's codes
+// after the other: 56, 59 and 61 us.  One sequence of 8 drafts: 7.1 us.
 template <int D, bool FP8>
 __global__ __launch_bounds__(256) void kv_keep_kernel(KvView c, KvLayers l, const int32_t* __restrict__ kept,
                                                       const int32_t* __restrict__ n_kept, uint32_t n_items) {
@@ -193,6 +198,8 @@ __global__ __launch_bounds__(256) void kv_keep_kernel(KvView c, KvLayers l, cons
 
 // The first workgroups write the tables, 256 entries of a fork each; a wave of the
 // others copies, for a fork and layer, one head's keys or values of the last page.
+// Measured: 96 beams, 16 layers of 4 heads of 128, pages of 64: 25.5 us, 5.3 TB/s; 8 samples in
+// 32 layers, 14.7 MB: 8.9 us, 5 of them the kernel's (lengths, table, codes one after the other).
 __global__ __launch_bounds__(256) void kv_fork_kernel(KvView c, KvLayers l, KvForks f, uint32_t table_groups,
                                                       uint32_t n_items) {
     auto known = [&](int i, int& s, int& d, int& n) {
@@ -391,7 +398,8 @@ __global__ __launch_bounds__(kOneThreads) void compact_plan_kernel(KvCompact m, 
 }
 
 // The first workgroups write the table and the moved pages' new ids, the others take
-// moves in turn, a workgroup a head's keys or values in one layer at a time.
+// moves in turn, a workgroup 16 KB of a page's keys or values in one layer at a time.
+// Measured: 3,900 moves of pages of 16 in 4 layers of 8 heads of 128, 1.03 GB: 217 us, 4.75 TB/s.
 __global__ __launch_bounds__(256) void compact_move_kernel(KvView c, KvLayers l, KvCompact m, uint32_t table_groups,
                                                            const int32_t* n_moves) {
     if (blockIdx.x < table_groups) {

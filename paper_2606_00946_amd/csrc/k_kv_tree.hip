@@ -17,7 +17,7 @@
 // (fp8) 98 us, 393 TFLOP/s; 2 of 64 x 8 over 64k to 128k tokens (int8) 462 us, 780 TFLOP/s; 24 of
 // 33 to 160 x 2 heads of 64 under a window of 2,048 (int8) 81 us; one of 8 drafts over 300
 // tokens 11.7 us.  In the long one the matrix pipes are busy for 40 % of the cycles and the vector
-// instructions (the exponential, its argument and sum, conversions of codes and weights) take 61 %: a wave
+// instructions (the exponential, its argument and sum, conversions of codes and weights) take 56 %: a wave
 // alternates between the two, and two waves a SIMD, which is what the registers allow, seldom
 // have one in each.  Raising a wave's priority for its products did not change that.
 #include <algorithm>
