@@ -494,6 +494,10 @@ def test_refusals(ctx):
             bad = (lodestar.ls_kv_cache * 2).from_buffer_copy(lay.caches.c)
             setattr(bad[1], name, getattr(bad[0], name))
             refused("twice", call(c=bad))
+    many = type(batch.c).from_buffer_copy(batch.c)
+    many.n_seqs = 2 ** 24
+    refused("too large", keep(b=ctypes.byref(many)), lodestar.LS_ERR_UNSUPPORTED)
+    refused("too large", fork(m=2 ** 24), lodestar.LS_ERR_UNSUPPORTED)
     refused("batch must", keep(b=None))
     refused("kept", keep(k=None))
     refused("n_kept", keep(m=None))

@@ -399,7 +399,7 @@ def test_refusals(ctx):
     out = torch.full_like(q, 5.0)
     lib = lodestar.library()
 
-    def refused(word, tree=None, batch=None, **a):
+    def refused(word, tree=None, batch=None, code=lodestar.LS_ERR_INVALID, **a):
         t, b = type(s.tree.c).from_buffer_copy(s.tree.c), type(s.batch.c).from_buffer_copy(s.batch.c)
         b.dtype = lodestar.LS_BF16
         for n, x in (tree or {}).items():
@@ -410,9 +410,10 @@ def test_refusals(ctx):
         g.update(a)
         rc = lib.ls_kv_attention_tree(ctx.h, s.cache.ref, ctypes.byref(b), None if tree == {} else ctypes.byref(t), g["q"],
                                       g["qs"], g["hq"], g["scale"], g["window"], g["sinks"], g["o"], g["os"], None)
-        assert rc == lodestar.LS_ERR_INVALID and word in ctx.last_error(), (rc, ctx.last_error())
+        assert rc == code and word in ctx.last_error(), (rc, ctx.last_error())
 
     note("kv tree refusals")
+    refused("too large", batch=dict(n_tokens=2 ** 29), code=lodestar.LS_ERR_UNSUPPORTED)
     refused("tree must", tree={})
     refused("mask must", tree=dict(mask=None))
     refused("mask_words", tree=dict(mask_words=1))
