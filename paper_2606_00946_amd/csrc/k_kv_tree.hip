@@ -688,12 +688,18 @@ hipError_t launch_kv_tree(const KvView& c, const KvTree& t, const void* q, int64
     a.mask = t.mask;
     a.words = t.words;
     a.pos = t.pos;
-    // Tiles of 64 rows halve the conversions and the codes' way from the caches, but leave half as many workgroups something
-    // to do and less room for codes on their way.  Measured with 32 and 64, 8 kv heads of 128, us: 32 sequences of 2,000
-    // tokens with 48 rows 33 and 62, 96 rows 57 and 50, 256 rows 115 and 94; 4 of 16,000 with 128 rows 61 and 104, 512 rows
-    // 159 and 171; 2 of 88,000 with 512 rows 530 and 455.
+    // Tiles of 64 rows halve the conversions and the codes' way from the caches, and leave half as many workgroups something
+    // to do: worth it once tiles of 32 are more than fit the device at one time.  Measured with 32 and 64, 8 kv heads of 128
+    // where nothing else is said, us: 16 sequences of 2,000 tokens with 128 rows (512 tiles of 32) 33 and 57, 20 of them
+    // (640) 66 and 43; 32 with 48 rows (512) 33 and 62, 50 with 64 rows (800) 70 and 52; 128 of 1,000 with 36 rows 91 and 64;
+    // 80 with 128 rows, 2 heads (640) 72 and 49; 8 of 4,000 with 128 rows, 16 heads (512) 48 and 78, 32 heads (1,024) 103
+    // and 90; 20 with 128 rows of 64 dimensions (640) 42 and 33.  Half-filled tiles can lose: 10 of 4,000 with 66 rows, 32
+    // heads 110 and 128.  Lengths are on the device: of uneven ones a last tile is taken to be half full.  Over very long
+    // caches the conversions count alone: 4 of 16,000 with 512 rows 152 and 161; 2 of 88,000 with 512 rows 530 and 455.
     const int64_t all_rows = (int64_t)c.T * a.G, most_rows = (int64_t)c.max_new * a.G;
-    const bool wide = c.D != 256 && ((most_rows > 64 && all_rows >= 3072) || (most_rows >= 256 && all_rows * c.limit >= 1 << 26));
+    const int64_t tiles32 = std::min(all_rows / 32 + c.B / 2, (most_rows + 31) / 32 * c.B);
+    const bool wide = c.D != 256 && ((most_rows > 32 && tiles32 * c.H > (int64_t)n_cu * 2) ||
+                                     (most_rows >= 256 && all_rows * c.limit >= 1 << 26));
     const int rows = wide ? 64 : 32;
     const int64_t tiles = (int64_t)c.T * a.G / rows + c.B;
     const int64_t line = ((int64_t)c.limit / (16 * kUnit) + 2 + kTreeStart) * c.H;

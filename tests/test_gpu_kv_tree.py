@@ -84,6 +84,22 @@ def test_rows_and_words(ctx, n, G):
     check(ctx, grown(Setup([(past, n) for past in (0, 1, 15, 16, 40, 64)], H=1, seed=n + G), extra_words=n % 2), G)
 
 
+@pytest.mark.parametrize("D,fmt,kind", [(128, "fp8", "bf16"), (128, "int8", "f16"), (64, "int8", "bf16"), (64, "fp8", "f16"),
+                                        (256, "fp8", "bf16")])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (40, 5)])
+def test_many_tiles(ctx, D, fmt, kind, window, sinks):
+    """More row tiles of heads than workgroups that fit the device, with pages that are not there."""
+    note(f"kv tree many tiles D={D} {fmt} {kind} window={window}")
+    check(ctx, grown(Setup(SEQS, H=8, D=D, fmt=fmt, kind=kind, seed=23, absent=((2, 3), (6, 0))), extra_words=1), 16, window, sinks)
+
+
+@pytest.mark.parametrize("n", [8, 9, 16, 17])
+@pytest.mark.parametrize("B", [15, 16, 17, 70])
+def test_tiles_around_what_fits(ctx, B, n):
+    note(f"kv tree {B} sequences of {n}")
+    check(ctx, grown(Setup([(50 * b % 130, n) for b in range(B)], H=16, D=64, seed=B + n)), 4)
+
+
 def test_chain_is_causal_attention(ctx):
     """A chain of drafts sees what causal attention shows it: the two calls agree."""
     import torch
