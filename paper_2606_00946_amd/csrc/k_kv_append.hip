@@ -216,9 +216,10 @@ __device__ __forceinline__ void append_row(const KvView& c, const KvRope& r, con
 
 // A page and head's keys or values in general.  A lane holds D / 64 units of a
 // 16-token block: keys a rotary unit of one token, values four dimensions of four
-// tokens.  A page of one block (ONE; `turns`: its positions' table rows)
-// stays in registers between finding the scale and writing the codes; larger ones
-// are read again, from the caches.
+// tokens.  New rows of one block (ONE; `turns`: its positions' table rows) stay in
+// registers between finding the scale and writing the codes; those of several are
+// read again, from the caches (pages of 32 and 64, an axis for each pair, 4 tokens of each of 9
+// sequences 12.3 and 8.7 us, 8 of each of 32 10.6 and 8.3).
 template <int D, bool FP8, bool F16, bool VALUE, bool ONE, Where AT>
 __device__ __forceinline__ void append_page(const KvView& c, const KvRope& r, const KvPositions& at, const PageWork& w, int h,
                                             const Turn (&turns)[D / 64]) {
@@ -227,7 +228,7 @@ __device__ __forceinline__ void append_page(const KvView& c, const KvRope& r, co
     float* sp = (VALUE ? c.vs : c.ks) + w.page * c.H + h;
     uint8_t* base = (VALUE ? c.v : c.k) + block_at(c, w.page, h, 0);
     const float held = w.row0 > 0 ? *sp : 0.0f;
-    const int b0 = ONE ? 0 : w.row0 >> 4, b1 = ONE ? 1 : (w.row1 + 15) >> 4;
+    const int b0 = w.row0 >> 4, b1 = ONE ? b0 + 1 : (w.row1 + 15) >> 4;
     const uint16_t* src = w.src + h * D;
     float x[N][16];
     auto load = [&](int blk) {
@@ -364,12 +365,13 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvView c, KvRope r, KvPo
                 return;
             }
             Turn turns[D / 64] = {};
-            if (c.page == 16) {
+            const int row = p.row0 & ~15;
+            if (p.row1 <= row + 16) {
                 if constexpr (!V)
 #pragma unroll
                     for (int i = 0; i < D / 64; ++i) {
                         const int e = i * 64 + lane;
-                        turns[i] = turn_at<AT>(r, at, unit_of(r, e % U), e % U, p.pos0 + e / U, p.row_of(e / U), c.T);
+                        turns[i] = turn_at<AT>(r, at, unit_of(r, e % U), e % U, p.pos0 + row + e / U, p.row_of(row + e / U), c.T);
                     }
                 for (int i = 0; i < hn; ++i) append_page<D, FP8, F16, V, true, AT>(c, r, at, p, h0 + i, turns);
             } else {
