@@ -608,7 +608,8 @@ int ls_kv_read(ls_ctx* ctx, const ls_kv_cache* cache, const ls_kv_batch* batch, 
  * own ancestors, and keeps one path.  ls_kv_append_at and ls_kv_attention_tree
  * work on one layer's cache like the calls above, the others on all layers'
  * caches in one call: `caches` is a host array of n_caches of them, all with the
- * same dtype, n_kv_heads, head_dim, page_tokens and n_pages, and none twice.
+ * same dtype, n_kv_heads, head_dim, page_tokens and n_pages, and none twice: no two of
+ * their arrays, codes or scales, may overlap.
  *
  * ls_positions  positions of the call's rows for the rotation (host struct):
  *   n_axes       1..LS_MAX_AXES

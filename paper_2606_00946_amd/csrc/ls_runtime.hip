@@ -15,6 +15,7 @@
 
 #include "ls_internal.h"
 #include "ls_kv_calls.h"
+#include "ls_kv_ranges.h"
 #include "ls_scratch.h"
 #include "k_policy.h"
 
@@ -106,6 +107,7 @@ struct ls_ctx {
     // shared_start: the start is the stop of the record before it (its
     // owner), so it is released and destroyed with that record only
     struct Rec { int kind; hipEvent_t start, stop; bool shared_start; };
+    std::vector<ls::KvRange> kv_ranges;      // of a call's caches, while it checks them
     std::vector<Rec> recs;
     std::vector<hipEvent_t> spare;
     hipEvent_t last_stop = nullptr;          // stop of the group timed last, while the next may follow it
@@ -1445,10 +1447,28 @@ int kv_layers(ls_ctx* c, const ls_kv_cache* caches, int32_t n, ls::KvView* v) {
         if (a.dtype != b.dtype || a.n_kv_heads != b.n_kv_heads || a.head_dim != b.head_dim ||
             a.page_tokens != b.page_tokens || a.n_pages != b.n_pages)
             return fail(c, LS_ERR_INVALID, "the caches must have the same dtype, heads, dimensions, page tokens and pages");
-        // a cache that is given twice would be rewritten by two waves at once
-        for (int32_t j = 0; j < i; ++j)
-            if (caches[j].k == b.k || caches[j].v == b.v) return fail(c, LS_ERR_INVALID, "a cache is given twice");
     }
+    return LS_OK;
+}
+
+// Every array of every cache is rewritten by waves of its own: one that is given twice, as two layers' codes or
+// scales or as one's keys and values, would be rewritten by two at once.
+int kv_apart(ls_ctx* c, const ls_kv_cache* caches, int32_t n, const ls::KvView& v) {
+    const int64_t scales = v.n_pages * v.H, codes = scales * v.page * v.D;
+    try {
+        c->kv_ranges.resize((size_t)n * 4);
+    } catch (const std::bad_alloc&) {
+        return fail(c, LS_ERR_NOMEM, "no host memory for the ranges of %d caches", n);
+    }
+    ls::KvRange* r = c->kv_ranges.data();
+    for (int32_t i = 0; i < n; ++i) {
+        *r++ = ls::kv_range(caches[i].k, codes);
+        *r++ = ls::kv_range(caches[i].v, codes);
+        *r++ = ls::kv_range(caches[i].k_scale, scales * 4);
+        *r++ = ls::kv_range(caches[i].v_scale, scales * 4);
+    }
+    if (ls::kv_ranges_meet(c->kv_ranges.data(), (int64_t)n * 4))
+        return fail(c, LS_ERR_INVALID, "a cache is given twice, or two of the caches' arrays overlap");
     return LS_OK;
 }
 
@@ -1653,7 +1673,7 @@ int ls_kv_keep(ls_ctx* c, const ls_kv_cache* caches, int32_t n_caches, const ls_
     c->err.clear();
     ls::KvView w;
     int rc = kv_layers(c, caches, n_caches, &w);
-    if (rc || (rc = kv_view(c, caches, batch, &w, false))) return rc;
+    if (rc || (rc = kv_apart(c, caches, n_caches, w)) || (rc = kv_view(c, caches, batch, &w, false))) return rc;
     if (w.B == 0 || w.T == 0) return LS_OK;
     if (!kept || !n_kept) return fail(c, LS_ERR_INVALID, "kept and n_kept must be non-NULL");
     DeviceScope dev(c->device);
@@ -1674,7 +1694,7 @@ int ls_kv_fork(ls_ctx* c, const ls_kv_cache* caches, int32_t n_caches, int32_t n
     c->err.clear();
     ls::KvView w{};
     int rc = kv_layers(c, caches, n_caches, &w);
-    if (rc || (rc = kv_table(c, w, n_rows, pages_stride))) return rc;
+    if (rc || (rc = kv_apart(c, caches, n_caches, w)) || (rc = kv_table(c, w, n_rows, pages_stride))) return rc;
     if (n_forks < 0) return fail(c, LS_ERR_INVALID, "n_forks must be >= 0");
     if (n_forks == 0 || n_rows == 0) return LS_OK;
     if (!pages || !pages_out || !src || !dst || !tokens)
@@ -1702,6 +1722,7 @@ int ls_kv_compact(ls_ctx* c, const ls_kv_cache* caches, int32_t n_caches, int32_
         return fail(c, LS_ERR_INVALID, "pages, pages_out, where and n_used must be non-NULL");
     if (ls::kv_compact_bytes(w.n_pages) > (int64_t)LS_KV_WORKSPACE_BYTES - ls::kKvCountBytes)
         return fail(c, LS_ERR_UNSUPPORTED, "the workspace holds the moves of a pool of up to 16 million pages");
+    if ((rc = kv_apart(c, caches, n_caches, w))) return rc;
     DeviceScope dev(c->device);
     if (!dev.ok) return fail(c, LS_ERR_DEVICE, "cannot select device %d", c->device);
     hipStream_t s = (hipStream_t)stream;
