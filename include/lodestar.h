@@ -637,7 +637,8 @@ int ls_kv_read(ls_ctx* ctx, const ls_kv_cache* cache, const ls_kv_batch* batch, 
  *   entry that does not, or is no new token of the sequence.  A token whose old or new page is absent
  *   stays where it is.  A page that tokens move into gets the larger of its scale and the one that the largest
  *   magnitude among them asks for (ls_kv_append's rule, the division by 127 as a product with 1 / 127 in fp32), and
- *   what it holds up to the last kept token is brought to it; codes are rounded once more where the scales differ.
+ *   what it holds up to the last kept token is brought to it; codes are rounded once more where the scales differ,
+ *   and stay as they are, whatever they are, in tokens that do not move on pages whose scale stays.
  *   What lies behind the last kept token is nobody's.  As with ls_kv_append, no two sequences of a call may share a
  *   page from past[b] on.
  * ls_kv_fork  for i < n_forks, row dst[i] of pages_out takes over the first tokens[i] tokens of row src[i] of
