@@ -130,6 +130,9 @@ __device__ __forceinline__ void keep_rows(const KvView& c, uint8_t* codes, float
         }
         if (!any) continue;
         const float scale = fmaxf(kept_scale<FP8>(wave_max(top)), held), inv = 1.0f / scale;
+        // what a code of token t is to be multiplied by; finite, since a token of zeros asks for no scale: from the largest
+        // onto the smallest it would be infinite
+        auto again = [&](int t) { return fminf(from[t] * inv, 0x1p+64f); };
         int loaded = b1 - 1;
         for (int blk = scale > held ? 0 : b0; blk < b1; ++blk) {
             if (blk != loaded) load(blk);
@@ -143,7 +146,7 @@ __device__ __forceinline__ void keep_rows(const KvView& c, uint8_t* codes, float
                     for (int d = 0; d < ND; ++d) {
                         uint4v o;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) o[e] = regraded<FP8>(x[0][d][e], from[0] * inv);
+                        for (int e = 0; e < 4; ++e) o[e] = regraded<FP8>(x[0][d][e], again(0));
                         *reinterpret_cast<uint4v*>(p + d * 1024 + first * 64 + (lane & 3) * 16) = o;
                     }
                 }
@@ -163,7 +166,7 @@ __device__ __forceinline__ void keep_rows(const KvView& c, uint8_t* codes, float
                             uint32_t w = 0;
 #pragma unroll
                             for (int t = 0; t < 4; ++t)
-                                w |= (regraded<FP8>(x[t][d][e], from[t] * inv) & 255u) << 8 * t;
+                                w |= (regraded<FP8>(x[t][d][e], again(t)) & 255u) << 8 * t;
                             o[e] = (w & m) | (old[e] & ~m);
                         }
                         *at = o;

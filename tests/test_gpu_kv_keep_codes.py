@@ -43,3 +43,29 @@ def test_tokens_that_stay_keep_their_codes(ctx, past, path, D, page, fmt, odd): 
             np.testing.assert_array_equal(row(codes, t), row(before[name], t), err_msg=f"{name}: token {t} stays")
         for i, k in enumerate(path):
             np.testing.assert_array_equal(row(codes, past + i), row(before[name], past + k), err_msg=f"{name}: token {past + k} moves")
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("D,page", [(64, 16), (128, 32), (256, 16)])
+def test_zeros_between_the_ends_of_the_scales(ctx, D, page, fmt):  # noqa: F811
+    """A token of zeros on a page of the largest scale moves onto one of the smallest, a page of zeros: it stays zero."""
+    import torch
+    lay = Layers(8, layers=1, H=2, D=D, page=page, fmt=fmt, seed=D, spread=0.0)
+    past, n, path = page - 4, page + 4, [0, 1, 9, 12]            # kept tokens 9 and 12 lie on the second page
+    table = lay.rng.permutation(8)[:2]
+    codes, scales = ([lay.bufs[0][i + c].view(torch.uint8 if i == 0 else torch.float32).view(8, 2, -1) for c in range(2)] for i in (0, 2))
+    for c, s in zip(codes, scales):
+        c[table[0]] = 0
+        s[table[0]], s[table[1]] = 2.0 ** -64, 2.0 ** 64
+    for c, name in zip(codes, "kv"):
+        at = ko.offsets(page, D, name == "v")
+        for k in path:
+            c[table[(past + k) // page]][:, torch.from_numpy(at[(past + k) % page]).cuda()] = 0
+    want = [x.clone() for x in (*codes, *scales)]
+    kept = np.full(n, -1)
+    kept[:4] = path
+    note(f"kv keep zeros D={D} page={page} {fmt}")
+    ctx.ls_kv_keep(lay.caches, lodestar.KVBatch(i32([0, n]), i32([past]), i32(table[None]), n), i32(kept), i32([4]))
+    torch.cuda.synchronize()
+    for x, y in zip(want, (*codes, *scales)):
+        assert torch.equal(x, y)
