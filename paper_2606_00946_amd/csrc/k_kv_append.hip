@@ -508,12 +508,6 @@ hipError_t launch_kv_append_at(const KvView& c, const KvRope& r, const KvPositio
     });
 }
 
-hipError_t launch_kv_append(const KvView& c, const KvRope& r, const void* k, int64_t k_stride, const void* v,
-                            int64_t v_stride, const void* q, int64_t q_stride, int32_t Hq, void* q_out,
-                            int64_t q_out_stride, int n_cu, hipStream_t s) {
-    return launch_kv_append_at(c, r, KvPositions{}, k, k_stride, v, v_stride, q, q_stride, Hq, q_out, q_out_stride, n_cu, s);
-}
-
 hipError_t launch_kv_read(const KvView& c, void* k_out, void* v_out, hipStream_t s) {
     const int64_t n_items = ((int64_t)(c.T >> 4) + 2 * (int64_t)c.B) * c.H * 2;
     const int64_t groups = (n_items + 3) / 4;

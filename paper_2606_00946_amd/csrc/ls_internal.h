@@ -384,9 +384,6 @@ struct KvRope {
     const float *cos, *sin;
     int32_t n_pos, rotary, interleaved;
 };
-hipError_t launch_kv_append(const KvView& c, const KvRope& r, const void* k, int64_t k_stride, const void* v,
-                            int64_t v_stride, const void* q, int64_t q_stride, int32_t Hq, void* q_out,
-                            int64_t q_out_stride, int n_cu, hipStream_t s);
 hipError_t launch_kv_read(const KvView& c, void* k_out, void* v_out, hipStream_t s);
 hipError_t launch_kv_workspace_init(void* workspace, hipStream_t s);
 hipError_t launch_kv_attention(const KvView& c, const void* q, int64_t q_stride, int32_t Hq, float scale,
