@@ -8,6 +8,8 @@
 namespace ls {
 namespace {
 
+// A call.  The sums of what is cut, and their counts, lie as each kernel has them; kv_tree_kernel has no use for the fields
+// marked with a star, but runs 2 to 3 % slower over small and windowed trees if the arguments behind them lie elsewhere.
 struct AttnArgs {
     const uint16_t* q;
     uint16_t* out;
@@ -15,12 +17,13 @@ struct AttnArgs {
     int32_t G;                       // query heads of a kv head
     float scale2;                    // softmax scale * log2 e
     int32_t window, sinks;
-    int32_t few;                     // sequences with up to this many rows (new tokens x G) split along the keys
-    // segments (sequence, kv head) that are cut: sums of each part, and counts of those that are there
-    float* part_o;                   // [parts][16][D]
-    float2v* part_ml;                // [parts][16] running maximum and sum
-    uint32_t* arrived;               // [parts][2], zero between launches
-    // tiles of many rows whose tokens several workgroups share: [tile][share][kTileRows]
+    int32_t few;                     // *sequences with up to this many rows (new tokens x G) split along the keys
+    // Segments (sequence, kv head) that are cut into parts: [parts][16 rows], and two counts each.  Trees: stretches that
+    // hold pieces of heads, [2 fit][32 or 64 rows], and four counts for each stretch.
+    float* part_o;                   // [...][D]
+    float2v* part_ml;                // a row's reference and sum
+    uint32_t* arrived;               // counts of parts that are there, zero between launches
+    // *tiles of many rows whose tokens several workgroups share: [tile][share][kTileRows]
     float* tile_o;
     float2v* tile_ml;
 };
