@@ -8,24 +8,13 @@
 namespace ls {
 namespace {
 
-// A call.  The sums of what is cut, and their counts, lie as each kernel has them; kv_tree_kernel has no use for the fields
-// marked with a star, but runs 2 to 3 % slower over small and windowed trees if the arguments behind them lie elsewhere.
-struct AttnArgs {
+struct AttnCall {
     const uint16_t* q;
     uint16_t* out;
     int64_t q_stride, out_stride;
     int32_t G;                       // query heads of a kv head
     float scale2;                    // softmax scale * log2 e
     int32_t window, sinks;
-    int32_t few;                     // *sequences with up to this many rows (new tokens x G) split along the keys
-    // Segments (sequence, kv head) that are cut into parts: [parts][16 rows], and two counts each.  Trees: stretches that
-    // hold pieces of heads, [2 fit][32 or 64 rows], and four counts for each stretch.
-    float* part_o;                   // [...][D]
-    float2v* part_ml;                // a row's reference and sum
-    uint32_t* arrived;               // counts of parts that are there, zero between launches
-    // *tiles of many rows whose tokens several workgroups share: [tile][share][kTileRows]
-    float* tile_o;
-    float2v* tile_ml;
 };
 
 // What a sequence's rows see, in 16-token blocks: the first n_sink and those from
@@ -35,7 +24,7 @@ struct Span {
     __device__ __forceinline__ int32_t tile(int32_t i) const { return i < n_sink ? i : win + (i - n_sink); }
 };
 
-__device__ __forceinline__ Span span_of(const KvView& c, const AttnArgs& a, int32_t past, int32_t rows) {
+__device__ __forceinline__ Span span_of(const KvView& c, const AttnCall& a, int32_t past, int32_t rows) {
     const int32_t end = min(past + rows, c.limit);
     const int32_t lo = a.window > 0 ? min(max(past + 1 - a.window, 0), end) : 0;
     Span s;
@@ -57,7 +46,7 @@ struct Sight {
     int32_t last, gone, sink;
     __device__ __forceinline__ bool sees(int i) const { return (i <= last) & ((i > gone) | (i < sink)); }
 };
-__device__ __forceinline__ Sight sight(const AttnArgs& a, int32_t page, int32_t pos, int32_t tok) {
+__device__ __forceinline__ Sight sight(const AttnCall& a, int32_t page, int32_t pos, int32_t tok) {
     Sight s;
     s.last = page < 0 ? -1 : pos - tok;
     s.gone = a.window > 0 ? max(pos - a.window, -1) - tok : -1;
@@ -69,7 +58,7 @@ __device__ __forceinline__ Sight sight(const AttnArgs& a, int32_t page, int32_t 
 // before `end` that some row sees, `lo` being where the window of the first row
 // starts.  The others belong to nobody or are hidden, and may be NaN.
 __device__ __forceinline__ uint32_t first_bytes(int32_t n) { return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1; }
-__device__ __forceinline__ uint32_t kept_bytes(const AttnArgs& a, int32_t tok, int32_t lo, int32_t end) {
+__device__ __forceinline__ uint32_t kept_bytes(const AttnCall& a, int32_t tok, int32_t lo, int32_t end) {
     uint32_t m = first_bytes(end - tok);
     if (a.window > 0) m &= ~first_bytes(lo - tok) | first_bytes(a.sinks - tok);
     return m;

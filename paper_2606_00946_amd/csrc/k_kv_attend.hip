@@ -22,6 +22,17 @@
 namespace ls {
 namespace {
 
+struct AttnArgs : AttnCall {
+    int32_t few;                     // sequences with up to this many rows (new tokens x G) split along the keys
+    // segments (sequence, kv head) that are cut: sums of each part, and counts of those that are there
+    float* part_o;                   // [parts][16][D]
+    float2v* part_ml;                // [parts][16] running maximum and sum
+    uint32_t* arrived;               // [parts][2], zero between launches
+    // tiles of many rows whose tokens several workgroups share: [tile][share][kTileRows]
+    float* tile_o;
+    float2v* tile_ml;
+};
+
 constexpr int kFewRows = 16;         // rows of a kv head that split_part takes
 // Workgroups of kv_split_kernel on a compute unit, by its registers.
 template <int D>

@@ -31,11 +31,23 @@ namespace {
 
 using float16v = float __attribute__((ext_vector_type(16)));
 
-struct TreeArgs : AttnArgs {
-    const uint64_t* mask;
-    int32_t words;
-    const int32_t* pos;
+// What lies before a chunk of 64 sequences: workgroups, and those of cut lines.
+struct TreeChunk {
+    int64_t groups, cut;
+};
+
+struct TreeArgs : AttnCall {
     int32_t fit;                     // workgroups that fit the device
+    int32_t words;
+    // stretches of lines that are cut: two slots each for pieces' sums, and four counts (TreeWork::join)
+    float* part_o;                   // [2 fit][ROWS][D]
+    float2v* part_ml;                // [2 fit][ROWS] a row's reference and sum
+    uint32_t* arrived;               // [fit][4], zero between launches
+    // of many sequences, by kv_tree_plan_kernel: what a workgroup has of a line, and what lies before each chunk
+    float* each;
+    TreeChunk* chunk;                // [chunks + 1]
+    const uint64_t* mask;
+    const int32_t* pos;
     int64_t groups;                  // no more have work
 };
 
@@ -50,7 +62,7 @@ struct TreeSeq {
     int32_t t0, n, past, units, tiles;
 };
 template <int ROWS>
-__device__ __forceinline__ TreeSeq tree_seq(const KvView& c, const AttnArgs& a, int b) {
+__device__ __forceinline__ TreeSeq tree_seq(const KvView& c, const TreeArgs& a, int b) {
     TreeSeq s;
     seq_rows(c, b, s.t0, s.n);
     s.past = past_of(c, b);
@@ -121,8 +133,27 @@ struct TreeStretch {
 
 constexpr int kTries = 6;
 
-// The piece at hand.
-template <int ROWS>
+// What a workgroup has of a line in a try, when lines are `all` long in all, each times its tiles; whether it is the
+// last one, which cuts nothing and needs no look at what it gives.
+__device__ __forceinline__ bool tree_try(int pass, float all, float tiles, float fit, float& each) {
+    if (pass < kTries) {
+        each = all / fmaxf(fit - tiles * (0.3f + 0.7f / (kTries - 1) * (float)pass), 0.0f);
+    } else if (pass == kTries) {
+        each = 2.0f * all / fit;
+    } else {
+        each = INFINITY;
+        return true;
+    }
+    return false;
+}
+
+// The length of a line's stretches where a workgroup has `each` of it.
+__device__ __forceinline__ int32_t tree_per(int32_t units, int32_t heads, float length, float each, float fit) {
+    return tree_stretch(units, heads, max((int32_t)fminf(ceilf(length / each), fit), 1));
+}
+
+// The piece at hand.  PLANNED: kv_tree_plan_kernel has been over the sequences.
+template <int ROWS, bool PLANNED>
 struct TreeWork {
     const KvView& c;
     const TreeArgs& a;
@@ -136,22 +167,41 @@ struct TreeWork {
     __device__ __forceinline__ bool find(int64_t index) {
         const int lane = here(threadIdx.x & 63);
         auto seq_at = [&](int b) { return b < c.B ? tree_seq<ROWS>(c, a, b) : TreeSeq{0, 0, 0, 0, 0}; };
-        const TreeSeq early = seq_at(lane);          // of the first 64 sequences, a lane each
         const float fit = (float)a.fit;
         float all = 0.0f, each = 0.0f, tiles = 0.0f;
         bool found = false;
+        int first = 0;                               // sequences that are passed over, and what lies before them
+        TreeChunk before{0, 0};
+        TreeSeq early;                               // of the first 64 sequences, a lane each
+        if constexpr (PLANNED) {
+            const int chunks = (c.B + 63) >> 6;
+            if (a.chunk[chunks].groups <= index) return false;
+            int lo = 0, n = chunks;                  // the last chunk that starts at or before `index`, 64 ways at a time
+            while (n > 1) {
+                const int step = (n + 63) >> 6, i = lane * step;
+                const uint64_t m = __ballot(i < n && a.chunk[lo + i].groups <= index);
+                const int k = 63 - __clzll((long long)m);
+                lo += k * step;
+                n = min(step, n - k * step);
+            }
+            first = of(lo) * 64;
+            before = a.chunk[of(lo)];
+            each = *a.each;
+            found = true;
+        } else {
+            early = seq_at(lane);
+        }
         // first the sums, then some tries, then the workgroup's place; one body for all: the code's own length is what it
         // costs
 #pragma clang loop unroll(disable)
-        for (int pass = 0;; ++pass) {
-            int64_t groups = 0, cut = 0;             // workgroups, and those of cut lines
+        for (int pass = PLANNED ? kTries + 1 : 0;; ++pass) {
+            int64_t groups = before.groups, cut = before.cut;        // workgroups, and those of cut lines
 #pragma clang loop unroll(disable)
-            for (int b0 = 0; b0 < c.B; b0 += 64) {
-                const TreeSeq s = b0 == 0 ? early : seq_at(b0 + lane);
+            for (int b0 = first; b0 < c.B; b0 += 64) {
+                const TreeSeq s = !PLANNED && b0 == 0 ? early : seq_at(b0 + lane);
                 const int32_t length = (s.units + kTreeStart) * c.H;
                 if (pass == 0) all += wave_sum((float)length * (float)s.tiles);
-                const int32_t want = max((int32_t)fminf(ceilf((float)length / each), fit), 1);
-                const int32_t per = pass == 0 ? length : tree_stretch(s.units, c.H, want);
+                const int32_t per = pass == 0 ? length : tree_per(s.units, c.H, (float)length, each, fit);
                 const int32_t w = (int32_t)((uint32_t)(length + per - 1) / (uint32_t)per), mine = w * s.tiles;
                 const int32_t upto = (int32_t)wave_scan((uint32_t)mine), cuts = (int32_t)wave_scan(w > 1 ? (uint32_t)mine : 0u);
                 const uint64_t here_it_is = found ? __ballot(groups + upto > index) : 0;
@@ -187,14 +237,7 @@ struct TreeWork {
                 found = true;
                 continue;
             }
-            if (pass < kTries) {
-                each = all / fmaxf(fit - tiles * (0.3f + 0.7f / (kTries - 1) * (float)pass), 0.0f);
-            } else if (pass == kTries) {
-                each = 2.0f * all / fit;
-            } else {
-                each = INFINITY;                     // nothing is cut
-                found = true;
-            }
+            if (tree_try(pass, all, tiles, fit, each)) found = true;
         }
     }
     // The next piece; whether there is one.
@@ -244,14 +287,102 @@ struct TreeWork {
     }
 };
 
-template <int D, bool FP8, int NR>
+// Sequences that every workgroup goes through by itself; more go through kv_tree_plan_kernel, a launch that takes 6 us
+// for these.  Without and with it, 8 drafts each over 500 tokens, us: 8 kv heads of 128: 96 sequences 31 and 38, 128 36
+// and 42, 192 68 and 67, 512 183 and 145; one of 64: 128 13 and 19, 192 18.0 and 18.9, 256 23 and 19.
+constexpr int kFewSeqs = 128;
+
+// The search of TreeWork::find for many sequences, where going through all of them in every workgroup takes as
+// long as their number squared (4,096 of 8 drafts x 8 heads, one kv head 7.1 ms instead of 0.21; 65,536 of one draft
+// 707 ms instead of 1.1): one workgroup finds what each of the others has and where the chunks start.
+constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
+template <int ROWS>
+__global__ __launch_bounds__(kPlanThreads) void kv_tree_plan_kernel(KvView c, TreeArgs a) {
+    __shared__ float lengths[kPlanWaves];
+    __shared__ TreeChunk chunks[kPlanWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float fit = (float)a.fit;
+    // a sequence's workgroups, those of a cut line, and its line times its tiles
+    auto seq = [&](int b, float each, float& length) {
+        const TreeSeq s = b < c.B ? tree_seq<ROWS>(c, a, b) : TreeSeq{0, 0, 0, 0, 0};
+        const int32_t line = (s.units + kTreeStart) * c.H, per = tree_per(s.units, c.H, (float)line, each, fit);
+        const int32_t w = (int32_t)((uint32_t)(line + per - 1) / (uint32_t)per);
+        length = (float)line * (float)s.tiles;
+        return TreeChunk{(int64_t)w * s.tiles, w > 1 ? (int64_t)w * s.tiles : 0};
+    };
+    auto wave_total = [](TreeChunk x) {
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) {
+            x.groups += __shfl_xor(x.groups, o);
+            x.cut += __shfl_xor(x.cut, o);
+        }
+        return x;
+    };
+    float all;
+    auto totals = [&](float each) {
+        TreeChunk sum{0, 0};
+        float mine = 0.0f;
+        for (int b = threadIdx.x; b < c.B; b += kPlanThreads) {
+            float length;
+            const TreeChunk x = seq(b, each, length);
+            sum.groups += x.groups;
+            sum.cut += x.cut;
+            mine += length;
+        }
+        sum = wave_total(sum);
+        mine = wave_sum(mine);
+        __syncthreads();
+        if (lane == 0) {
+            chunks[wave] = sum;
+            lengths[wave] = mine;
+        }
+        __syncthreads();
+        sum = {0, 0};
+        all = 0.0f;
+        for (int w = 0; w < kPlanWaves; ++w) {
+            sum.groups += chunks[w].groups;
+            sum.cut += chunks[w].cut;
+            all += lengths[w];
+        }
+        return sum;
+    };
+    // as in find, but without tries that cannot succeed, since each tile takes a workgroup at least
+    float each = INFINITY;
+    const int64_t tiles = totals(each).groups;
+    if (tiles <= a.groups - a.fit)
+        for (int pass = tiles > a.fit ? kTries : 0;; ++pass) {
+            if (tree_try(pass, all, (float)tiles, fit, each)) break;
+            const TreeChunk x = totals(each);
+            if ((pass < kTries ? x.groups : x.cut) <= a.fit) break;
+        }
+    TreeChunk before{0, 0};
+    for (int b0 = 0; b0 < c.B; b0 += kPlanThreads) {
+        float length;
+        const TreeChunk x = wave_total(seq(b0 + threadIdx.x, each, length));
+        __syncthreads();
+        if (lane == 0) chunks[wave] = x;
+        __syncthreads();
+        for (int w = 0; w < kPlanWaves; ++w) {
+            const int i = (b0 >> 6) + w;
+            if (w == wave && lane == 0 && i * 64 < c.B) a.chunk[i] = before;
+            before.groups += chunks[w].groups;
+            before.cut += chunks[w].cut;
+        }
+    }
+    if (threadIdx.x == 0) {
+        a.chunk[(c.B + 63) >> 6] = before;
+        *a.each = each;
+    }
+}
+
+template <int D, bool FP8, int NR, bool PLANNED>
 __global__ __launch_bounds__(256, 2) void kv_tree_kernel(KvView c, TreeArgs a) {
     constexpr int ROWS = 32 * NR, ND = D / 64, NC = D / 32;
     constexpr bool HELD = D * NR <= 128;
     constexpr int DEPTH = D * NR <= 128 ? 2 : 1;         // steps whose codes are on their way
     __shared__ TreeLds<D, NR> lds;
     __shared__ TreeStretch stretch[4];
-    TreeWork<ROWS> work{c, a, stretch[__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)]};
+    TreeWork<ROWS, PLANNED> work{c, a, stretch[__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)]};
     for (int64_t i = blockIdx.x; i < a.groups && work.find(i); i += gridDim.x) while (work.next()) {
         const int thread = here(threadIdx.x), lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
         const int col = lane & 31, hi = lane >> 5;
@@ -707,6 +838,11 @@ hipError_t launch_kv_tree(const KvView& c, const KvTree& t, const void* q, int64
     // workgroups that fit the device, as far as the workspace has two slots for each
     WsCarve ws{(char*)workspace, (size_t)workspace_bytes};
     a.arrived = ws.take<uint32_t>(kMaxParts * 2);
+    const bool planned = c.B > kFewSeqs;
+    if (planned) {
+        a.each = ws.take<float>(1);
+        a.chunk = ws.take<TreeChunk>((int64_t)(c.B + 63) / 64 + 1);
+    }
     const int64_t room = (workspace_bytes - (int64_t)ws.off - 512) / ((int64_t)rows * (c.D + 2) * 4 * 2);
     a.fit = (int32_t)std::min<int64_t>({(int64_t)n_cu * 2, room, kMaxParts / 2});
     a.part_ml = ws.take<float2v>((int64_t)a.fit * 2 * rows);
@@ -714,16 +850,23 @@ hipError_t launch_kv_tree(const KvView& c, const KvTree& t, const void* q, int64
     if (!ws.ok()) return hipErrorInvalidConfiguration;
     a.groups = tiles + a.fit;
     const int64_t wgs = std::min<int64_t>(a.groups, 1 << 20);
-    auto run = [&](auto d, auto fp8) {
-        constexpr int D = decltype(d)::value;
+    auto launch = [&](auto d, auto fp8, auto tiles_of) {
+        constexpr int D = decltype(d)::value, NR = decltype(tiles_of)::value;
         constexpr bool FP8 = decltype(fp8)::value;
-        if constexpr (D != 256)
-            if (rows == 64) {
-                kv_tree_kernel<D, FP8, 2><<<(uint32_t)wgs, 256, 0, s>>>(c, a);
-                return hipGetLastError();
-            }
-        kv_tree_kernel<D, FP8, 1><<<(uint32_t)wgs, 256, 0, s>>>(c, a);
+        if (!planned) {
+            kv_tree_kernel<D, FP8, NR, false><<<(uint32_t)wgs, 256, 0, s>>>(c, a);
+            return hipGetLastError();
+        }
+        kv_tree_plan_kernel<32 * NR><<<1, kPlanThreads, 0, s>>>(c, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        kv_tree_kernel<D, FP8, NR, true><<<(uint32_t)wgs, 256, 0, s>>>(c, a);
         return hipGetLastError();
+    };
+    auto run = [&](auto d, auto fp8) {
+        if constexpr (decltype(d)::value != 256)
+            if (rows == 64) return launch(d, fp8, std::integral_constant<int, 2>{});
+        return launch(d, fp8, std::integral_constant<int, 1>{});
     };
     auto by_dim = [&](auto fp8) {
         if (c.D == 64) return run(std::integral_constant<int, 64>{}, fp8);
