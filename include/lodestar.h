@@ -620,7 +620,9 @@ int ls_kv_read(ls_ctx* ctx, const ls_kv_cache* cache, const ls_kv_batch* batch, 
  *                (NULL: all by axis 0); copied before return
  * ls_tree  what the call's rows see of their sequence's new tokens (host struct of device arrays):
  *   mask         uint64 [n_tokens x mask_words], 64 * mask_words >= max_new: bit j % 64 of word j / 64 of a row says
- *                that it sees new token j of its sequence (bits from the sequence's new tokens on do not count)
+ *                that it sees new token j of its sequence (bits from the sequence's new tokens on do not count).
+ *                A window hides cached tokens only: where a chain of drafts is longer than it, the mask leaves out
+ *                the bits of ancestors behind it
  *   pos          int32 [n_tokens]: the rows' positions, for the window only (NULL without one); below past[b]
  *                counts as past[b]
  *

@@ -59,7 +59,7 @@ __device__ __forceinline__ uint32_t regraded(uint32_t w, float again) {
 }
 
 // The scale that a largest magnitude asks for; for int8 by one product with 1 / 127 as 32 bits
-// hold it, within 2^-23 of the quotient.
+// hold it, within 2^-23 of the quotient (64 sequences, 32 layers: 41.4 us, with the quotient 41.9).
 template <bool FP8>
 __device__ __forceinline__ float kept_scale(float a) {
     return FP8 ? scale_of<true>(a) : fminf(fmaxf(a * (1.0f / 127.0f), kScaleMin), kScaleMax);
@@ -179,14 +179,17 @@ __device__ __forceinline__ void keep_rows(const KvView& c, uint8_t* codes, float
 }
 
 // Waves: (layer, sequence, head, key or value).  Measured: 64 sequences of 16 to 64 drafts, up to 9
-// of them kept, 32 layers of 8 heads of 128 (int8): 52 us, where its bytes would take 4.  Vector
-// instructions take 62 % of the cycles (540 a wave, most of them for the 16 tokens of a block whichever
+// of them kept, 32 layers of 8 heads of 128 (int8): 48 us, where its bytes would take 4.  Vector
+// instructions take 64 % of the cycles (550 a wave, most of them for the 16 tokens of a block whichever
 // of them move), the chain list, table, codes the rest.  Waves that keep 2, 4 or 8 heads
 // in turn read lists and tables less often and decode only what moves, but wait for one head's codes
-// after the other: 56, 59 and 61 us.  One sequence of 8 drafts: 7.1 us.
+// after the other: 56, 59 and 61 us beside 52.  One sequence of 8 drafts: 7.5 us.  int8 has room for six
+// waves a SIMD (the same lists over and over: 41 us, with five 44); FP8 would spill.
 template <int D, bool FP8>
-__global__ __launch_bounds__(256, FP8 || D == 256 ? 1 : 6) void kv_keep_kernel(KvView c, KvLayers l, const int32_t* __restrict__ kept,
-                                                      const int32_t* __restrict__ n_kept, uint32_t n_items) {
+__global__ __launch_bounds__(256, FP8 || D == 256 ? 1 : 6) void kv_keep_kernel(KvView c, KvLayers l,
+                                                                               const int32_t* __restrict__ kept,
+                                                                               const int32_t* __restrict__ n_kept,
+                                                                               uint32_t n_items) {
     const uint32_t w = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
     if (w >= n_items) return;
     const int value = w & 1, h = (int)((w >> 1) % (uint32_t)c.H);

@@ -14,12 +14,15 @@
 // each operand made of them serves all rows; only the queries are in LDS.
 //
 // Measured, 8 kv heads: 32 sequences of 16 to 64 drafts x 4 heads of 128 over 64 to 8,192 tokens
-// (fp8) 98 us, 393 TFLOP/s; 2 of 64 x 8 over 64k to 128k tokens (int8) 462 us, 780 TFLOP/s; 24 of
-// 33 to 160 x 2 heads of 64 under a window of 2,048 (int8) 81 us; one of 8 drafts over 300
-// tokens 11.7 us.  In the long one the matrix pipes are busy for 40 % of the cycles and the vector
+// (fp8) 101 us, 382 TFLOP/s; 2 of 64 x 8 over 64k to 128k tokens (int8) 455 us, 798 TFLOP/s; 24 of
+// 33 to 160 x 2 heads of 64 under a window of 2,048 (int8) 80 us; one of 8 drafts over 300
+// tokens 11.8 us.  In the long one the matrix pipes are busy for 40 % of the cycles and the vector
 // instructions (the exponential, its argument and sum, conversions of codes and weights) take 56 %: a wave
 // alternates between the two, and two waves a SIMD, which is what the registers allow, seldom
-// have one in each.  Raising a wave's priority for its products did not change that.
+// have one in each.  Raising a wave's priority for its products did not change that.  256 dimensions:
+// 16 of 32 x 4 heads over 2,000 tokens 52 us, 2 of 64 x 8 over 30,000 268, the matrix pipes busy for 35 and 49 %.
+// Registers that do not fit (64 rows of 128 dimensions, and 256 dimensions) are read back between
+// pieces and in steps that a mask cuts, not in the others.
 #include <algorithm>
 
 #include "k_kv_attend.h"
@@ -131,6 +134,8 @@ struct TreeStretch {
     int32_t per, hi;                     // stretches' length; the stretch's end
 };
 
+// Tries, from a share of 0.3 of a stretch more for each tile to a whole one.  Straight to the whole one: 32 sequences
+// of 16 to 64 drafts over 64 to 8,192 tokens 101 us instead of 95, 2 of 64 over 60,000 162 instead of 153.
 constexpr int kTries = 6;
 
 // What a workgroup has of a line in a try, when lines are `all` long in all, each times its tiles; whether it is the
@@ -826,7 +831,9 @@ hipError_t launch_kv_tree(const KvView& c, const KvTree& t, const void* q, int64
     // 80 with 128 rows, 2 heads (640) 72 and 49; 8 of 4,000 with 128 rows, 16 heads (512) 48 and 78, 32 heads (1,024) 103
     // and 90; 20 with 128 rows of 64 dimensions (640) 42 and 33.  Half-filled tiles can lose: 10 of 4,000 with 66 rows, 32
     // heads 110 and 128.  Lengths are on the device: of uneven ones a last tile is taken to be half full.  Over very long
-    // caches the conversions count alone: 4 of 16,000 with 512 rows 152 and 161; 2 of 88,000 with 512 rows 530 and 455.
+    // caches the conversions count alone: 4 of 16,000 with 512 rows 152 and 161; 2 of 88,000 with 512 rows 530 and 455.  How
+    // long is taken from the table's width, which can be far more than is cached: 8 of 2,000 with 256 rows in tables of
+    // 2,064, 16,384 and 131,072 tokens 34, 33 and 66 (31 with 32), 8 of 16,000 in the last 173 (156).
     const int64_t all_rows = (int64_t)c.T * a.G, most_rows = (int64_t)c.max_new * a.G;
     const int64_t tiles32 = std::min(all_rows / 32 + c.B / 2, (most_rows + 31) / 32 * c.B);
     const bool wide = c.D != 256 && ((most_rows > 32 && tiles32 * c.H > (int64_t)n_cu * 2) ||

@@ -287,7 +287,7 @@ class Positions:
 
 class Tree:
     """What drafted rows see (ls_tree): mask int64 [T x words] on the device, bit j of a row: it sees its sequence's new
-    token j; pos int32 [T], the rows' positions, needed with a window."""
+    token j, whatever the window; pos int32 [T], the rows' positions, needed with a window."""
 
     def __init__(self, mask, pos=None):
         import torch
