@@ -293,9 +293,9 @@ struct TreeWork {
 };
 
 // Sequences that every workgroup goes through by itself; more go through kv_tree_plan_kernel, a launch that takes 6 us
-// for these.  Without and with it, 8 drafts each over 500 tokens, us: 8 kv heads of 128: 96 sequences 31 and 38, 128 36
-// and 42, 192 68 and 67, 512 183 and 145; one of 64: 128 13 and 19, 192 18.0 and 18.9, 256 23 and 19.
-constexpr int kFewSeqs = 128;
+// for these.  Without and with it, 8 drafts each over 500 tokens, us: 8 kv heads of 128: 128 sequences 36 and 42, 160 45
+// and 51, 192 68 and 67, 256 77 and 72, 512 183 and 145; one of 64: 128 13 and 19, 192 18 and 19, 256 23 and 19.
+constexpr int kFewSeqs = 192;
 
 // The search of TreeWork::find for many sequences, where going through all of them in every workgroup takes as
 // long as their number squared (4,096 of 8 drafts x 8 heads, one kv head 7.1 ms instead of 0.21; 65,536 of one draft

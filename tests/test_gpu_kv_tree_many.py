@@ -22,14 +22,14 @@ def ragged(B, seed, longest=90):
     return seqs
 
 
-@pytest.mark.parametrize("B", [127, 128, 129, 193, 1000, 4097])
+@pytest.mark.parametrize("B", [127, 129, 191, 192, 193, 1000, 4097])
 @pytest.mark.parametrize("D,G,fmt,kind", [(64, 2, "fp8", "bf16"), (128, 16, "int8", "f16")])
 def test_many_sequences(ctx, B, D, G, fmt, kind):  # noqa: F811
     note(f"kv tree many sequences B={B} D={D} G={G} {fmt} {kind}")
     check(ctx, grown(Setup(ragged(B, B + G), H=1, D=D, fmt=fmt, kind=kind, seed=B)), G)
 
 
-@pytest.mark.parametrize("B", [130, 700])
+@pytest.mark.parametrize("B", [130, 200, 700])
 @pytest.mark.parametrize("D,H,G", [(64, 4, 4), (128, 2, 8), (256, 2, 2)])
 @pytest.mark.parametrize("window,sinks", [(0, 0), (2500, 20)])
 def test_long_ones_among_them(ctx, B, D, H, G, window, sinks):  # noqa: F811
